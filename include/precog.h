@@ -31,6 +31,12 @@
  * and the memory-consolidation steps of SMC:
  *   precog_smc_route        two-stage cluster routing (Sec. 5.1)
  *   precog_smc_consolidate  semantic-state EMA (Sec. 5.3 Eq. smc-ema)
+ * a second kind of layer with a state to store and inject, for whole sequences
+ * and for single tokens of running sessions, and the scores of an answer:
+ *   precog_delta_encode / precog_delta_step  the gated delta rule
+ *   precog_conv_encode / precog_conv_step    its short causal convolution
+ *   precog_score_tokens     log probabilities of given tokens, entropies and
+ *                           top alternatives
  *
  * Conventions shared by every entry point
  *   - All tensor pointers are device pointers owned by the caller.  The
@@ -512,6 +518,173 @@ precog_status precog_smc_consolidate(void *states, precog_dtype state_dtype,
                                      precog_dtype contrib_dtype,
                                      const int32_t *target, int64_t C,
                                      double alpha, void *stream);
+
+/* ------------------------------------------------------------------------ */
+/* Gated delta rule: matrix states                                          */
+/* ------------------------------------------------------------------------ */
+
+typedef struct {
+    int64_t batch;    /* B: sequences (precog_delta_step: tokens, one per row) */
+    int64_t seqlen;   /* L: tokens of every sequence; with `starts` T: tokens
+                         of the packed axis (precog_delta_step: unread) */
+    int64_t k_heads;  /* query/key heads, >= 1 */
+    int64_t v_heads;  /* value heads, a multiple of k_heads: v_heads / k_heads
+                         consecutive value heads share one query/key head */
+    int64_t k_dim;    /* K: a multiple of 8, 8..128 */
+    int64_t v_dim;    /* V: a multiple of 8, 8..256 */
+    int64_t q_stride; /* elements between tokens of q, k and v; 0 = heads * */
+    int64_t k_stride; /* dim.  Multiples of 8, so that slices of one fused  */
+    int64_t v_stride; /* projection can be passed as they are.              */
+    int64_t h0_batch_stride; /* elements between state rows; 0 = v_heads*K*V */
+    int64_t hT_batch_stride; /* the same for hT (precog_delta_step: unread) */
+    precog_dtype in_dtype;    /* q, k, v: PRECOG_F32 or PRECOG_BF16 */
+    precog_dtype out_dtype;   /* o: PRECOG_F32 or PRECOG_BF16 */
+    precog_dtype state_dtype; /* state storage: PRECOG_F32 or PRECOG_F16;
+                                 running states are always fp32 */
+    int32_t qk_norm;  /* nonzero: q and k of every head are first divided by
+                         sqrt(sum of squares + eps) */
+    float eps;        /* >= 0, read with qk_norm */
+    float scale;      /* factor of o; 0 = 1 / sqrt(k_dim) */
+} precog_delta_desc;
+
+/* The gated delta rule: the second kind of layer whose state can be stored
+ * and injected as in Sec. 4.2.  Each value head keeps a [K, V] matrix that
+ * forgets by a_t = exp(g_t) and has its value for key k_t replaced by v_t to
+ * the part beta_t:
+ *
+ *   u_t = beta_t (v_t - (a_t S_{t-1})^T k_t)
+ *   S_t = a_t S_{t-1} + k_t u_t^T
+ *   o_t = scale * S_t^T q_t,     hT = the state after the last token.
+ *
+ * Like the scan it is a rollout S(h0, x_1:L), so S(h0, c ++ q) =
+ * S(S(h0, c), q) holds for it too.
+ *   q, k       [B, L, k_heads, K], v [B, L, v_heads, V] in desc->in_dtype.
+ *   g, beta    [B, L, v_heads] fp32, or NULL for g = 0 / beta = 1.  g is the
+ *              log decay; g below -256 (-infinity too) erases the state.
+ *   starts     NULL, or [B + 1] int32 on the device: the sequences then lie
+ *              one behind the other in q, k, v, g, beta and o of T tokens,
+ *              sequence b in [starts[b], starts[b+1]), of any length (0 too).
+ *              Entries are clamped to [0, T], an end before its begin is an
+ *              empty sequence, and rows of o in no sequence are left as they
+ *              are.  Sequences must not overlap.
+ *   h0         state rows [v_heads, K, V] in desc->state_dtype at
+ *              desc->h0_batch_stride; NULL = zero initial states.
+ *   h0_idx     NULL: sequence b starts from row b of h0.  Else [B] int32 on
+ *              the device: from row h0_idx[b] of the h0_rows rows of h0 (the
+ *              injection of a retrieved state, without a copy of it); an
+ *              index outside [0, h0_rows) reads nothing and starts from NaN.
+ *   o          [B, L, v_heads, V] in desc->out_dtype; NULL = states only
+ *              (then q is not read and may be NULL).
+ *   hT         state rows like h0, or NULL.  May equal h0 exactly without
+ *              h0_idx (in place); must not overlap h0 otherwise.
+ * Arithmetic in fp32.  A NaN or an infinity in a token reaches o of its head
+ * and sequence from the beginning of the token's block of 32 on.
+ * Alignment: pointers 16 bytes (g, beta, starts, h0_idx: 4), strides as above.
+ * Deterministic; nothing but o and hT is written. */
+precog_status precog_delta_encode(const precog_delta_desc *desc, const void *q,
+                                  const void *k, const void *v, const float *g,
+                                  const float *beta, const int32_t *starts,
+                                  const void *h0, int64_t h0_rows,
+                                  const int32_t *h0_idx, void *o, void *hT,
+                                  void *stream);
+
+/* One token of each of desc->batch running sessions: the rule above for a
+ * single t, the state of row i being row slots[i] of `states`, updated in
+ * place.
+ *   q, k, v, g, beta, o   as above for B tokens: [B, heads, dim], [B, v_heads]
+ *   states     [state_rows, v_heads, K, V] in desc->state_dtype, row stride
+ *              desc->h0_batch_stride
+ *   slots      [B] int32 on the device, B <= 65535.  A slot outside
+ *              [0, state_rows) updates nothing and leaves its row of o as it
+ *              is (rows of a padded batch).  Rows with the same slot are
+ *              applied in the order of the rows (F16 states rounded after
+ *              each), as separate calls would.
+ * All in fp32 except the storage types.  Deterministic. */
+precog_status precog_delta_step(const precog_delta_desc *desc, const void *q,
+                                const void *k, const void *v, const float *g,
+                                const float *beta, void *states,
+                                int64_t state_rows, const int32_t *slots,
+                                void *o, void *stream);
+
+/* ------------------------------------------------------------------------ */
+/* Short causal convolution                                                 */
+/* ------------------------------------------------------------------------ */
+
+typedef struct {
+    int64_t batch;    /* B: sequences (precog_conv_step: tokens, one per row) */
+    int64_t seqlen;   /* L, or with `starts` T, as in precog_delta_desc */
+    int64_t dim;      /* D: channels, a multiple of 8 */
+    int64_t width;    /* W: taps, 2, 3 or 4 */
+    int64_t x_stride; /* elements between tokens of x; 0 = D; multiple of 8 */
+    precog_dtype in_dtype;  /* x and tails: PRECOG_F32 or PRECOG_BF16 */
+    precog_dtype out_dtype; /* y: PRECOG_F32 or PRECOG_BF16 */
+    int32_t silu;     /* nonzero: y = silu(sum), else y = sum */
+} precog_conv_desc;
+
+/* The causal depthwise convolution of Table 1 (the last W inputs of every
+ * channel) with its tail, the last W - 1 inputs, as a state that is injected
+ * and captured beside the layer's recurrent one:
+ *
+ *   y_t[d] = act(bias[d] + sum_{j<W} w[d, j] x_{t-W+1+j}[d])
+ *
+ * where x before a sequence's first token is its tail (oldest first).
+ *   x          [B, L, D] in desc->in_dtype     y [B, L, D] in desc->out_dtype
+ *   w          [D, W] fp32     bias [D] fp32 or NULL
+ *   starts     as in precog_delta_encode
+ *   tail0      [rows, W - 1, D] in desc->in_dtype, or NULL (zeros); row b, or
+ *              row tail_idx[b] of tail_rows rows ([B] int32 on the device; an
+ *              index outside the rows: NaN)
+ *   tailT      [B, W - 1, D]: the last W - 1 of tail0's and the sequence's
+ *              inputs; NULL = not captured.  May equal tail0 exactly without
+ *              tail_idx; must not overlap it otherwise.
+ * fp32 sums in the order of the taps.  y must not overlap x.  Pointers 16-byte
+ * aligned (starts and tail_idx: 4). */
+precog_status precog_conv_encode(const precog_conv_desc *desc, const void *x,
+                                 const float *w, const float *bias,
+                                 const int32_t *starts, const void *tail0,
+                                 int64_t tail_rows, const int32_t *tail_idx,
+                                 void *y, void *tailT, void *stream);
+
+/* The same for one token of each of desc->batch sessions: y [B, D] from x
+ * [B, D] and the tails in row slots[i] of tails [tail_rows, W - 1, D], which
+ * move on by one input in place.  Slots as in precog_delta_step. */
+precog_status precog_conv_step(const precog_conv_desc *desc, const void *x,
+                               const float *w, const float *bias, void *tails,
+                               int64_t tail_rows, const int32_t *slots,
+                               void *y, void *stream);
+
+/* ------------------------------------------------------------------------ */
+/* Scores of answer tokens                                                  */
+/* ------------------------------------------------------------------------ */
+
+/* Bytes of device workspace precog_score_tokens needs: 0 unless few long
+ * rows are each read by several workgroups.  0 for arguments it refuses. */
+size_t precog_score_workspace_bytes(int64_t T, int64_t V, int64_t top);
+
+/* Log probabilities under softmax(logits) of each of T rows over V tokens:
+ *   logprob[t]  = x[token[t]] - log sum_v exp(x[v])
+ *   entropy[t]  = -sum_v p_v log p_v  (0 for p_v = 0)
+ *   top_id[t], top_logprob[t]  the `top` largest logits, best first, equal
+ *                 logits in the order of their ids, with their log p
+ *   logits     [T, V] in logits_dtype (F32, BF16 or F16), rows row_stride
+ *              elements apart (0 = V); any V, any stride >= V
+ *   token      [T] int32 on the device, or NULL (then logprob is unread)
+ *              token < 0: the row has no token, logprob 0; token >= V: -inf
+ *   logprob    [T] fp32     entropy [T] fp32 or NULL
+ *   top_id     [T, top] int32, top_logprob [T, top] fp32; 0 <= top <= 64
+ * -infinity is a masked token: it has probability zero and is no alternative;
+ * alternatives beyond the unmasked ones have id -1 and -infinity.  A row with
+ * nothing unmasked has logprob -infinity and entropy 0.  A row with a NaN or a
+ * +infinity has NaN in all its numbers and ids of -1.  Sums in fp32.
+ *   workspace  precog_score_workspace_bytes(T, V, top) bytes
+ * T, V < 2^31; logits aligned as their type, workspace 16 bytes, others 4. */
+precog_status precog_score_tokens(const void *logits, precog_dtype logits_dtype,
+                                  int64_t T, int64_t V, int64_t row_stride,
+                                  const int32_t *token, int64_t top,
+                                  float *logprob, float *entropy,
+                                  int32_t *top_id, float *top_logprob,
+                                  void *workspace, size_t workspace_bytes,
+                                  void *stream);
 
 /* Static, human-readable name of a status code. */
 const char *precog_status_string(precog_status s);

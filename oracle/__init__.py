@@ -24,6 +24,9 @@ What each function follows in the paper (arXiv 2608.02560):
 * ``route2``, ``ema``, ``consolidate`` -- SMC two-stage routing (Sec. 5.1,
   Eqs. smc-domain, smc-sub) and semantic EMA consolidation (Sec. 5.3,
   Eq. smc-ema), one update and a chunk-ordered sequence of them.
+* ``delta``, ``conv``, ``score`` -- the gated delta rule, the short causal
+  convolution (Table 1) and the log probabilities, entropies and alternatives
+  of rows of logits.
 * ``round_bf16``, ``round_f16`` -- round-to-nearest-even storage rounding of
   fp64 values (the paper stores states at FP16, Sec. 4.2).
 """
@@ -69,6 +72,9 @@ def _load():
         lib.oracle_scan_complex_f64.restype = ctypes.c_int
         lib.oracle_top1_f64.argtypes = [i64, i64, i64, fp, fp, ip, dp, ctypes.c_int]
         lib.oracle_top1_f64.restype = ctypes.c_int
+        lib.oracle_delta_f64.argtypes = [i64] * 5 + [dp] * 7 + [ctypes.c_int] + \
+            [ctypes.c_double] * 2
+        lib.oracle_delta_f64.restype = ctypes.c_int
         _lib = lib
     return _lib
 
@@ -291,6 +297,68 @@ def consolidate(states, contrib, target, alpha):
         if 0 <= r < out.shape[0]:
             out[r] = ema(out[r], h[c], alpha)
     return out
+
+
+def delta(q, k, v, g=None, beta=None, h0=None, qk_norm=False, eps=1e-6, scale=None):
+    """The gated delta rule over one sequence, token after token in fp64: q, k
+    [T, Hk, K] (q None: states only), v [T, Hv, V], g and beta [T, Hv], h0
+    [Hv, K, V] (None: zeros).  Returns (o [T, Hv, V] or None, hT)."""
+    q, k, v, g, beta, h0 = (_f64(t) for t in (q, k, v, g, beta, h0))
+    (T, Hk, K), (Hv, V) = k.shape, v.shape[1:]
+    assert v.shape[0] == T and (q is None or q.shape == k.shape)
+    S = np.zeros((Hv, K, V)) if h0 is None else h0.copy()
+    assert S.shape == (Hv, K, V)
+    o = np.zeros((T, Hv, V)) if q is not None else None
+    rc = _load().oracle_delta_f64(T, Hk, Hv, K, V, _ptr(q), _ptr(k), _ptr(v), _ptr(g), _ptr(beta),
+                                  _ptr(S), _ptr(o), int(bool(qk_norm)), float(eps),
+                                  float(K ** -0.5 if scale is None else scale))
+    assert rc == 0, rc
+    return o, S
+
+
+def conv(x, w, bias=None, tail=None, silu=True):
+    """The causal depthwise convolution of one sequence in fp64: x [T, D], w
+    [D, W], bias [D], tail [W - 1, D] (None: zeros).  Returns (y, new tail)."""
+    x, w, bias, tail = (_f64(t) for t in (x, w, bias, tail))
+    W = w.shape[1]
+    if tail is None:
+        tail = np.zeros((W - 1, w.shape[0]))
+    ext = np.concatenate([tail, x])
+    y = np.zeros_like(x)
+    for t in range(x.shape[0]):
+        for j in range(W):
+            y[t] += w[:, j] * ext[t + j]
+    if bias is not None:
+        y = y + bias
+    if silu:
+        with np.errstate(over="ignore"):
+            y = y / (1.0 + np.exp(-y))
+    return y, ext[ext.shape[0] - (W - 1):]
+
+
+def score(x, token=None, top=0):
+    """One row of logits x [V] in fp64: (log p of token, entropy, ids, log p of
+    the `top` best).  -inf is masked; a NaN or +inf spoils the row."""
+    x = _f64(x)
+    V = x.shape[0]
+    ids, lps = np.full(top, -1), np.full(top, -np.inf)
+    if np.isnan(x).any() or (x == np.inf).any():
+        return np.nan, np.nan, ids, np.full(top, np.nan)
+    live = np.flatnonzero(x > -np.inf)
+    none = token is not None and token < 0
+    if live.size == 0:
+        return (0.0 if none else -np.inf), 0.0, ids, lps
+    m = x[live].max()
+    log_z = np.log(np.exp(x[live] - m).sum())  # of x - m: m itself may swallow it
+    lp = (x[live] - m) - log_z
+    entropy = -(np.exp(lp) * lp).sum()
+    best = live[np.lexsort((live, -x[live]))][:top]
+    ids[:best.size] = best
+    lps[:best.size] = (x[best] - m) - log_z
+    given = 0.0 if none else -np.inf
+    if token is not None and 0 <= token < V:
+        given = (x[token] - m) - log_z
+    return given, entropy, ids, lps
 
 
 def round_bf16(a):

@@ -24,6 +24,8 @@
  *                       A_k = a_k + i w_k (a_k > 0 in this sign convention):
  *                       complex state, real input term, readout of the real
  *                       part of C_t . h_t.
+ *   oracle_delta_f64    the gated delta rule over one sequence, from and to
+ *                       matrix states.
  *
  * Rows (b, d) of the scan are independent (the recurrence is diagonal in the
  * state, Eq. 1), so the driver may hand disjoint row ranges to threads; each
@@ -318,5 +320,69 @@ int oracle_top1_f64(int64_t Q, int64_t M, int64_t E, const float *q,
         pthread_join(th[i], NULL);
     free(th);
     free(jobs);
+    return 0;
+}
+
+/* ------------------------------------------------------------------------- */
+/* Gated delta rule                                                           */
+/* ------------------------------------------------------------------------- */
+
+/* One sequence of T tokens, every value head in turn:
+ *   u = beta_t (v_t - (a_t S)^T k_t),  S <- a_t S + k_t u^T,  a_t = exp(g_t),
+ *   o_t = scale S^T q_t
+ * q, k : [T, Hk, K], v : [T, Hv, V], g, beta (nullable: 0, 1) : [T, Hv],
+ * S : [Hv, K, V] initial state in, final state out, o (nullable) : [T, Hv, V].
+ * Head h reads query/key head h / (Hv / Hk); norm divides q and k of a token
+ * and head by sqrt(sum of squares + eps). */
+int oracle_delta_f64(int64_t T, int64_t Hk, int64_t Hv, int64_t K, int64_t V, const double *q,
+                     const double *k, const double *v, const double *g, const double *beta,
+                     double *S, double *o, int norm, double eps, double scale)
+{
+    if (T < 0 || Hk < 1 || Hv < 1 || Hv % Hk || K < 1 || V < 1 || !S || (T > 0 && (!k || !v)) ||
+        (T > 0 && o && !q))
+        return 1;
+    double *kn = (double *)malloc(sizeof(double) * K);
+    double *qn = (double *)malloc(sizeof(double) * K);
+    if (!kn || !qn) {
+        free(kn);
+        free(qn);
+        return 4;
+    }
+    for (int64_t h = 0; h < Hv; ++h) {
+        double *Sh = S + h * K * V;
+        const int64_t hk = h / (Hv / Hk);
+        for (int64_t t = 0; t < T; ++t) {
+            const double *kt = k + (t * Hk + hk) * K;
+            const double *qt = o ? q + (t * Hk + hk) * K : NULL;
+            const double *vt = v + (t * Hv + h) * V;
+            double k2 = 0.0, q2 = 0.0;
+            for (int64_t i = 0; i < K; ++i) {
+                k2 += kt[i] * kt[i];
+                if (qt)
+                    q2 += qt[i] * qt[i];
+            }
+            for (int64_t i = 0; i < K; ++i) {
+                kn[i] = norm ? kt[i] / sqrt(k2 + eps) : kt[i];
+                qn[i] = !qt ? 0.0 : norm ? qt[i] / sqrt(q2 + eps) : qt[i];
+            }
+            const double a = g ? exp(g[t * Hv + h]) : 1.0;
+            const double b = beta ? beta[t * Hv + h] : 1.0;
+            for (int64_t j = 0; j < V; ++j) {
+                double seen = 0.0;
+                for (int64_t i = 0; i < K; ++i)
+                    seen += a * Sh[i * V + j] * kn[i];
+                const double u = b * (vt[j] - seen);
+                double out = 0.0;
+                for (int64_t i = 0; i < K; ++i) {
+                    Sh[i * V + j] = a * Sh[i * V + j] + kn[i] * u;
+                    out += Sh[i * V + j] * qn[i];
+                }
+                if (o)
+                    o[(t * Hv + h) * V + j] = scale * out;
+            }
+        }
+    }
+    free(kn);
+    free(qn);
     return 0;
 }

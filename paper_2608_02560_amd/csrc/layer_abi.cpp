@@ -1,0 +1,342 @@
+// C-ABI layer of the gated-delta rule, its convolution and token scoring
+// (include/precog.h): host-side validation and launches.  Nothing here
+// allocates, copies between host and device or synchronises.
+#include <cmath>
+
+#include <hip/hip_runtime.h>
+
+#include "layer_kernels.h"
+
+namespace {
+
+bool aligned(const void* p, uintptr_t to) {
+  return (reinterpret_cast<uintptr_t>(p) & (to - 1)) == 0;
+}
+
+constexpr int64_t kMaxTokens = 0x7fffffffLL;  // of one call: positions are int32
+constexpr int64_t kMaxStride = 1LL << 24;     // elements between tokens: 32 of them stay below 2^31 bytes
+
+int size_of(precog_dtype t) { return t == PRECOG_F32 ? 4 : 2; }
+
+bool valid_io(precog_dtype t) { return t == PRECOG_F32 || t == PRECOG_BF16; }
+
+// [a, a + an) and [b, b + bn) share a byte
+bool overlap(const void* a, size_t an, const void* b, size_t bn) {
+  const uintptr_t x = reinterpret_cast<uintptr_t>(a), y = reinterpret_cast<uintptr_t>(b);
+  return an && bn && x < y + bn && y < x + an;
+}
+
+// Status of a finished launch.
+precog_status launched(hipError_t e) { return e == hipSuccess ? PRECOG_OK : PRECOG_ERR_HIP; }
+
+precog_status validate_delta(const precog_delta_desc* d, bool step) {
+  if (!d) return PRECOG_ERR_NULL;
+  if (d->batch < 0 || (!step && d->seqlen < 0)) return PRECOG_ERR_SHAPE;
+  if (d->batch > kMaxTokens || (!step && d->seqlen > kMaxTokens)) return PRECOG_ERR_SHAPE;
+  if (step && d->batch > 65535) return PRECOG_ERR_SHAPE;
+  if (d->k_heads < 1 || d->v_heads < 1 || d->k_heads > 65535 || d->v_heads > 65535 ||
+      d->v_heads % d->k_heads != 0)
+    return PRECOG_ERR_SHAPE;
+  if (d->k_dim < 8 || d->k_dim > precog::kDeltaMaxK || d->k_dim % 8 != 0) return PRECOG_ERR_SHAPE;
+  if (d->v_dim < 8 || d->v_dim > precog::kDeltaMaxV || d->v_dim % 8 != 0) return PRECOG_ERR_SHAPE;
+  if (!(d->eps >= 0.f) || !std::isfinite(d->eps) || !std::isfinite(d->scale)) return PRECOG_ERR_SHAPE;
+  if (!valid_io(d->in_dtype) || !valid_io(d->out_dtype)) return PRECOG_ERR_DTYPE;
+  if (d->state_dtype != PRECOG_F32 && d->state_dtype != PRECOG_F16) return PRECOG_ERR_DTYPE;
+  const int64_t kd = d->k_heads * d->k_dim, vd = d->v_heads * d->v_dim, sd = vd * d->k_dim;
+  if (kd > kMaxStride || vd > kMaxStride) return PRECOG_ERR_SHAPE;
+  const struct { int64_t stride, least; } token[] = {{d->q_stride, kd}, {d->k_stride, kd}, {d->v_stride, vd}};
+  for (const auto& t : token) {
+    if (t.stride == 0) continue;
+    if (t.stride < t.least || t.stride > kMaxStride) return PRECOG_ERR_STRIDE;
+    if (t.stride % 8 != 0) return PRECOG_ERR_ALIGN;
+  }
+  for (const int64_t s : {d->h0_batch_stride, d->hT_batch_stride}) {
+    if (s == 0) continue;
+    if (s < sd || s > (1LL << 40)) return PRECOG_ERR_STRIDE;
+    if (s % 8 != 0) return PRECOG_ERR_ALIGN;
+  }
+  return PRECOG_OK;
+}
+
+precog::DeltaParams delta_params(const precog_delta_desc* d, const void* q, const void* k,
+                                 const void* v, const float* g, const float* beta, void* o) {
+  precog::DeltaParams p{};
+  const int64_t kd = d->k_heads * d->k_dim, vd = d->v_heads * d->v_dim;
+  p.q = q;
+  p.k = k;
+  p.v = v;
+  p.g = g;
+  p.beta = beta;
+  p.o = o;
+  p.B = d->batch;
+  p.q_stride = d->q_stride ? d->q_stride : kd;
+  p.k_stride = d->k_stride ? d->k_stride : kd;
+  p.v_stride = d->v_stride ? d->v_stride : vd;
+  p.h0_stride = d->h0_batch_stride ? d->h0_batch_stride : vd * d->k_dim;
+  p.hT_stride = d->hT_batch_stride ? d->hT_batch_stride : vd * d->k_dim;
+  p.Hk = static_cast<int>(d->k_heads);
+  p.Hv = static_cast<int>(d->v_heads);
+  p.K = static_cast<int>(d->k_dim);
+  p.V = static_cast<int>(d->v_dim);
+  p.norm = d->qk_norm != 0;
+  p.eps = d->eps;
+  p.scale = d->scale != 0.f ? d->scale : 1.f / std::sqrt(static_cast<float>(d->k_dim));
+  return p;
+}
+
+precog_status validate_conv(const precog_conv_desc* d, bool step) {
+  if (!d) return PRECOG_ERR_NULL;
+  if (d->batch < 0 || d->dim < 0 || (!step && d->seqlen < 0)) return PRECOG_ERR_SHAPE;
+  if (d->batch > kMaxTokens || d->dim > kMaxStride || (!step && d->seqlen > kMaxTokens))
+    return PRECOG_ERR_SHAPE;
+  if (step && d->batch > 65535) return PRECOG_ERR_SHAPE;
+  if (d->width < 2 || d->width > 4) return PRECOG_ERR_SHAPE;
+  if (!valid_io(d->in_dtype) || !valid_io(d->out_dtype)) return PRECOG_ERR_DTYPE;
+  if (d->x_stride != 0 && (d->x_stride < d->dim || d->x_stride > kMaxStride)) return PRECOG_ERR_STRIDE;
+  if (d->dim % 8 != 0 || d->x_stride % 8 != 0) return PRECOG_ERR_ALIGN;
+  return PRECOG_OK;
+}
+
+precog::ConvParams conv_params(const precog_conv_desc* d, const void* x, const float* w,
+                               const float* bias, void* y) {
+  precog::ConvParams p{};
+  p.x = x;
+  p.w = w;
+  p.bias = bias;
+  p.y = y;
+  p.B = d->batch;
+  p.D = d->dim;
+  p.x_stride = d->x_stride ? d->x_stride : d->dim;
+  p.W = static_cast<int>(d->width);
+  p.silu = d->silu != 0;
+  return p;
+}
+
+// Workgroups of one row of a scoring call: one when the rows alone give each
+// of the 256 CUs eight workgroups, else as many as bring the call there while
+// each keeps two tiles to read.
+int64_t score_splits(int64_t T, int64_t V) {
+  const int64_t tiles = (V + precog::kScoreTile - 1) / precog::kScoreTile;
+  const int64_t want = (8 * 256 + T - 1) / T;
+  const int64_t most = tiles / 2 < 64 ? tiles / 2 : 64;
+  const int64_t n = want < most ? want : most;
+  return n < 1 ? 1 : n;
+}
+
+bool valid_score(int64_t T, int64_t V, int64_t top) {
+  return T >= 0 && V >= 1 && T <= 0x7fffffffLL && V <= 0x7fffffffLL && top >= 0 &&
+         top <= precog::kScoreMaxTop;
+}
+
+struct ScoreWs {
+  size_t part, val, total;
+};
+ScoreWs score_ws(int64_t T, int64_t splits, int64_t top) {
+  ScoreWs w{0, 0, 0};
+  if (splits <= 1) return w;
+  const auto up = [](size_t v) { return (v + 255) & ~static_cast<size_t>(255); };
+  w.part = up(static_cast<size_t>(T) * splits * sizeof(precog::ScorePart));
+  w.val = up(static_cast<size_t>(T) * splits * top * 4);
+  w.total = w.part + 2 * w.val;
+  return w;
+}
+
+}  // namespace
+
+extern "C" {
+
+precog_status precog_delta_encode(const precog_delta_desc* desc, const void* q, const void* k,
+                                  const void* v, const float* g, const float* beta,
+                                  const int32_t* starts, const void* h0, int64_t h0_rows,
+                                  const int32_t* h0_idx, void* o, void* hT, void* stream) {
+  precog_status st = validate_delta(desc, false);
+  if (st != PRECOG_OK) return st;
+  const int64_t B = desc->batch, L = desc->seqlen;
+  const int64_t tokens = starts ? L : (L > 0 && B > kMaxTokens / L ? -1 : B * L);
+  if (tokens < 0) return PRECOG_ERR_SHAPE;
+  if (B * desc->v_heads > kMaxTokens / 8) return PRECOG_ERR_SHAPE;  // workgroups, 8 a head at most
+  if (B == 0) return PRECOG_OK;
+  const bool work = tokens > 0;
+  if (work && (!k || !v || (o && !q))) return PRECOG_ERR_NULL;
+  if ((!o || !work) && !hT) return PRECOG_OK;  // nothing requested
+  if (h0_idx && h0_rows < 0) return PRECOG_ERR_SHAPE;
+  if (h0_idx && h0_rows > 0 && !h0) return PRECOG_ERR_NULL;
+  for (const void* p : {q, k, v, h0, static_cast<const void*>(o), static_cast<const void*>(hT)})
+    if (!aligned(p, 16)) return PRECOG_ERR_ALIGN;
+  if (!aligned(g, 4) || !aligned(beta, 4) || !aligned(starts, 4) || !aligned(h0_idx, 4))
+    return PRECOG_ERR_ALIGN;
+
+  precog::DeltaParams p = delta_params(desc, q, k, v, g, beta, work ? o : nullptr);
+  p.starts = starts;
+  p.idx = h0_idx;
+  p.state_rows = h0_idx ? h0_rows : B;
+  p.h0 = h0;
+  p.hT = hT;
+  p.L = L;
+  p.T = tokens;
+  // hT over h0: in place, row for row, or not at all
+  const int64_t sd = desc->v_heads * desc->v_dim * desc->k_dim;
+  const size_t es = static_cast<size_t>(size_of(desc->state_dtype));
+  const int64_t rows = h0_idx ? h0_rows : B;
+  if (h0 && hT && rows > 0 &&
+      overlap(h0, ((rows - 1) * p.h0_stride + sd) * es, hT, ((B - 1) * p.hT_stride + sd) * es)) {
+    const bool layers = !h0_idx && p.h0_stride == p.hT_stride;  // slots of one multi-layer store
+    const auto a = reinterpret_cast<uintptr_t>(h0), b = reinterpret_cast<uintptr_t>(hT);
+    const size_t pitch = static_cast<size_t>(p.h0_stride) * es, one = static_cast<size_t>(sd) * es;
+    const size_t off = (a < b ? b - a : a - b) % pitch;
+    if (!layers || (h0 != hT && (off < one || off + one > pitch))) return PRECOG_ERR_STRIDE;
+  }
+  int cus = 1;
+  st = precog::check_device(&cus);
+  if (st != PRECOG_OK) return st;
+  (void)hipGetLastError();
+  return launched(precog::launch_delta(p, desc->in_dtype, desc->out_dtype, desc->state_dtype, cus,
+                                       static_cast<hipStream_t>(stream)));
+}
+
+precog_status precog_delta_step(const precog_delta_desc* desc, const void* q, const void* k,
+                                const void* v, const float* g, const float* beta, void* states,
+                                int64_t state_rows, const int32_t* slots, void* o, void* stream) {
+  precog_status st = validate_delta(desc, true);
+  if (st != PRECOG_OK) return st;
+  if (state_rows < 0) return PRECOG_ERR_SHAPE;
+  if (desc->batch == 0) return PRECOG_OK;
+  if (!k || !v || !slots || (o && !q) || (state_rows > 0 && !states)) return PRECOG_ERR_NULL;
+  for (const void* p : {q, k, v, static_cast<const void*>(states), static_cast<const void*>(o)})
+    if (!aligned(p, 16)) return PRECOG_ERR_ALIGN;
+  if (!aligned(g, 4) || !aligned(beta, 4) || !aligned(slots, 4)) return PRECOG_ERR_ALIGN;
+  if (state_rows == 0) return PRECOG_OK;  // no slot can name a row
+
+  precog::DeltaParams p = delta_params(desc, q, k, v, g, beta, o);
+  p.idx = slots;
+  p.state_rows = state_rows;
+  p.h0 = states;
+  p.hT = states;
+  int cus = 1;
+  st = precog::check_device(&cus);
+  if (st != PRECOG_OK) return st;
+  (void)hipGetLastError();
+  return launched(precog::launch_delta_step(p, desc->in_dtype, desc->out_dtype, desc->state_dtype,
+                                            cus, static_cast<hipStream_t>(stream)));
+}
+
+precog_status precog_conv_encode(const precog_conv_desc* desc, const void* x, const float* w,
+                                 const float* bias, const int32_t* starts, const void* tail0,
+                                 int64_t tail_rows, const int32_t* tail_idx, void* y, void* tailT,
+                                 void* stream) {
+  precog_status st = validate_conv(desc, false);
+  if (st != PRECOG_OK) return st;
+  const int64_t B = desc->batch, L = desc->seqlen, D = desc->dim;
+  const int64_t tokens = starts ? L : (L > 0 && B > kMaxTokens / L ? -1 : B * L);
+  if (tokens < 0) return PRECOG_ERR_SHAPE;
+  if (B == 0 || D == 0) return PRECOG_OK;
+  const bool work = tokens > 0;
+  if (work && !x) return PRECOG_ERR_NULL;
+  if (work && y && !w) return PRECOG_ERR_NULL;
+  if ((!y || !work) && !tailT) return PRECOG_OK;  // nothing requested
+  if (tail_idx && tail_rows < 0) return PRECOG_ERR_SHAPE;
+  if (tail_idx && tail_rows > 0 && !tail0) return PRECOG_ERR_NULL;
+  for (const void* p : {x, static_cast<const void*>(w), static_cast<const void*>(bias), tail0,
+                        static_cast<const void*>(y), static_cast<const void*>(tailT)})
+    if (!aligned(p, 16)) return PRECOG_ERR_ALIGN;
+  if (!aligned(starts, 4) || !aligned(tail_idx, 4)) return PRECOG_ERR_ALIGN;
+  const size_t row = static_cast<size_t>((desc->width - 1) * D) * size_of(desc->in_dtype);
+  const int64_t rows = tail_idx ? tail_rows : B;
+  if (tail0 && tailT && overlap(tail0, rows * row, tailT, B * row) && (tail_idx || tail0 != tailT))
+    return PRECOG_ERR_STRIDE;
+
+  precog::ConvParams p = conv_params(desc, x, w, bias, work ? y : nullptr);
+  p.starts = starts;
+  p.idx = tail_idx;
+  p.tail_rows = tail_idx ? tail_rows : B;
+  p.tail0 = tail0;
+  p.tailT = tailT;
+  p.L = L;
+  p.T = tokens;
+  int cus = 1;
+  st = precog::check_device(&cus);
+  if (st != PRECOG_OK) return st;
+  (void)hipGetLastError();
+  return launched(precog::launch_conv(p, desc->in_dtype, desc->out_dtype, cus,
+                                      static_cast<hipStream_t>(stream)));
+}
+
+precog_status precog_conv_step(const precog_conv_desc* desc, const void* x, const float* w,
+                               const float* bias, void* tails, int64_t tail_rows,
+                               const int32_t* slots, void* y, void* stream) {
+  precog_status st = validate_conv(desc, true);
+  if (st != PRECOG_OK) return st;
+  if (tail_rows < 0) return PRECOG_ERR_SHAPE;
+  if (desc->batch == 0 || desc->dim == 0) return PRECOG_OK;
+  if (!x || !slots || (y && !w) || (tail_rows > 0 && !tails)) return PRECOG_ERR_NULL;
+  for (const void* p : {x, static_cast<const void*>(w), static_cast<const void*>(bias),
+                        static_cast<const void*>(tails), static_cast<const void*>(y)})
+    if (!aligned(p, 16)) return PRECOG_ERR_ALIGN;
+  if (!aligned(slots, 4)) return PRECOG_ERR_ALIGN;
+  if (tail_rows == 0) return PRECOG_OK;
+  precog::ConvParams p = conv_params(desc, x, w, bias, y);
+  p.idx = slots;
+  p.tail_rows = tail_rows;
+  p.tail0 = tails;
+  p.tailT = tails;
+  st = precog::check_device(nullptr);
+  if (st != PRECOG_OK) return st;
+  (void)hipGetLastError();
+  return launched(precog::launch_conv_step(p, desc->in_dtype, desc->out_dtype,
+                                           static_cast<hipStream_t>(stream)));
+}
+
+size_t precog_score_workspace_bytes(int64_t T, int64_t V, int64_t top) {
+  if (!valid_score(T, V, top) || T == 0) return 0;
+  return score_ws(T, score_splits(T, V), top).total;
+}
+
+precog_status precog_score_tokens(const void* logits, precog_dtype logits_dtype, int64_t T,
+                                  int64_t V, int64_t row_stride, const int32_t* token, int64_t top,
+                                  float* logprob, float* entropy, int32_t* top_id,
+                                  float* top_logprob, void* workspace, size_t workspace_bytes,
+                                  void* stream) {
+  if (!valid_score(T, V, top)) return PRECOG_ERR_SHAPE;
+  if (logits_dtype != PRECOG_F32 && logits_dtype != PRECOG_BF16 && logits_dtype != PRECOG_F16)
+    return PRECOG_ERR_DTYPE;
+  if (row_stride != 0 && (row_stride < V || row_stride > (1LL << 40))) return PRECOG_ERR_STRIDE;
+  if (T == 0) return PRECOG_OK;
+  if (!logits || (token && !logprob) || (top > 0 && (!top_id || !top_logprob)))
+    return PRECOG_ERR_NULL;
+  if (!token && !entropy && top == 0) return PRECOG_OK;  // nothing requested
+  if (!aligned(logits, size_of(logits_dtype)) || !aligned(workspace, 16)) return PRECOG_ERR_ALIGN;
+  for (const void* p : {static_cast<const void*>(token), static_cast<const void*>(logprob),
+                        static_cast<const void*>(entropy), static_cast<const void*>(top_id),
+                        static_cast<const void*>(top_logprob)})
+    if (!aligned(p, 4)) return PRECOG_ERR_ALIGN;
+  const int64_t splits = score_splits(T, V);
+  const ScoreWs ws = score_ws(T, splits, top);
+  if (ws.total > 0 && (!workspace || workspace_bytes < ws.total)) return PRECOG_ERR_WORKSPACE;
+
+  precog::ScoreParams p{};
+  p.logits = logits;
+  p.token = token;
+  p.logprob = logprob;
+  p.entropy = entropy;
+  p.top_id = top_id;
+  p.top_logprob = top_logprob;
+  p.T = T;
+  p.V = V;
+  p.row_stride = row_stride ? row_stride : V;
+  p.top = static_cast<int>(top);
+  p.splits = static_cast<int>(splits);
+  const int64_t tiles = (V + precog::kScoreTile - 1) / precog::kScoreTile;
+  p.span = (tiles + splits - 1) / splits * precog::kScoreTile;
+  if (splits > 1) {
+    char* at = static_cast<char*>(workspace);
+    p.part = reinterpret_cast<precog::ScorePart*>(at);
+    p.cand_val = reinterpret_cast<float*>(at + ws.part);
+    p.cand_id = reinterpret_cast<int32_t*>(at + ws.part + ws.val);
+  }
+  const precog_status st = precog::check_device(nullptr);
+  if (st != PRECOG_OK) return st;
+  (void)hipGetLastError();
+  return launched(precog::launch_score(p, logits_dtype, static_cast<hipStream_t>(stream)));
+}
+
+}  // extern "C"

@@ -21,25 +21,6 @@ std::atomic<int> g_arch_ok[kMaxDevices];
 // compute units of each device (0 = not yet queried)
 std::atomic<int> g_cus[kMaxDevices];
 
-// Checks that the current device is a gfx950; `cus`, if given, receives its
-// compute-unit count.  Both are queried once per device and cached.
-precog_status check_device(int* cus = nullptr) {
-  int dev = 0;
-  if (hipGetDevice(&dev) != hipSuccess) return PRECOG_ERR_HIP;
-  if (dev < 0 || dev >= kMaxDevices) return PRECOG_ERR_ARCH;
-  int st = g_arch_ok[dev].load(std::memory_order_relaxed);
-  if (st == 0) {
-    hipDeviceProp_t prop;
-    if (hipGetDeviceProperties(&prop, dev) != hipSuccess) return PRECOG_ERR_HIP;
-    st = std::strncmp(prop.gcnArchName, "gfx950", 6) == 0 ? 1 : 2;
-    g_cus[dev].store(prop.multiProcessorCount > 0 ? prop.multiProcessorCount : 1,
-                     std::memory_order_relaxed);
-    g_arch_ok[dev].store(st, std::memory_order_relaxed);
-  }
-  if (cus) *cus = g_cus[dev].load(std::memory_order_relaxed);
-  return st == 1 ? PRECOG_OK : PRECOG_ERR_ARCH;
-}
-
 bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
 
 bool valid_n(int64_t n) {
@@ -51,6 +32,7 @@ constexpr int64_t kCus = precog::kShapeCus;
 static_assert(kBlock == precog::kShapeBlock, "the larger workgroup");
 
 using precog::ceil_div;
+using precog::check_device;
 using precog::lanes_per_row;
 using precog::scan_shape;
 using precog::ScanShape;
@@ -89,6 +71,28 @@ precog_status validate_desc(const precog_scan_desc* d) {
 }
 
 }  // namespace
+
+namespace precog {
+// Checks that the current device is a gfx950; `cus`, if given, receives its
+// compute-unit count.  Both are queried once per device and cached.
+precog_status check_device(int* cus) {
+  int dev = 0;
+  if (hipGetDevice(&dev) != hipSuccess) return PRECOG_ERR_HIP;
+  if (dev < 0 || dev >= kMaxDevices) return PRECOG_ERR_ARCH;
+  int st = g_arch_ok[dev].load(std::memory_order_relaxed);
+  if (st == 0) {
+    hipDeviceProp_t prop;
+    if (hipGetDeviceProperties(&prop, dev) != hipSuccess) return PRECOG_ERR_HIP;
+    st = std::strncmp(prop.gcnArchName, "gfx950", 6) == 0 ? 1 : 2;
+    g_cus[dev].store(prop.multiProcessorCount > 0 ? prop.multiProcessorCount : 1,
+                     std::memory_order_relaxed);
+    g_arch_ok[dev].store(st, std::memory_order_relaxed);
+  }
+  if (cus) *cus = g_cus[dev].load(std::memory_order_relaxed);
+  return st == 1 ? PRECOG_OK : PRECOG_ERR_ARCH;
+}
+
+}  // namespace precog
 
 extern "C" {
 

@@ -9,6 +9,10 @@
 
 namespace precog {
 
+// Checks that the current device is a gfx950; `cus`, if given, receives its
+// compute-unit count (precog_abi.cpp).
+precog_status check_device(int* cus = nullptr);
+
 // Storage tags.  bf16 and fp16 are both 16-bit; the tags keep them apart.
 struct bf16_t { uint16_t bits; };
 struct f16_t { uint16_t bits; };

@@ -33,7 +33,9 @@ EXPORTS = ("precog_scan_workspace_bytes", "precog_scan_encode", "precog_scan_enc
            "precog_retrieve_topk_prepared", "precog_query_workspace_bytes",
            "precog_query_top1_prefill", "precog_inject_gather", "precog_inject_compose",
            "precog_inject_fuse",
-           "precog_smc_route", "precog_smc_consolidate", "precog_status_string")
+           "precog_smc_route", "precog_smc_consolidate", "precog_delta_encode",
+           "precog_delta_step", "precog_conv_encode", "precog_conv_step",
+           "precog_score_workspace_bytes", "precog_score_tokens", "precog_status_string")
 
 
 class PrecogError(RuntimeError):
@@ -50,6 +52,23 @@ class ScanDesc(ctypes.Structure):
                 ("state_dtype", ctypes.c_int),
                 ("h0_batch_stride", ctypes.c_int64), ("hT_batch_stride", ctypes.c_int64),
                 ("chunk", ctypes.c_int64)]
+
+
+class DeltaDesc(ctypes.Structure):
+    _fields_ = [("batch", ctypes.c_int64), ("seqlen", ctypes.c_int64),
+                ("k_heads", ctypes.c_int64), ("v_heads", ctypes.c_int64),
+                ("k_dim", ctypes.c_int64), ("v_dim", ctypes.c_int64),
+                ("q_stride", ctypes.c_int64), ("k_stride", ctypes.c_int64),
+                ("v_stride", ctypes.c_int64), ("h0_batch_stride", ctypes.c_int64),
+                ("hT_batch_stride", ctypes.c_int64), ("in_dtype", ctypes.c_int),
+                ("out_dtype", ctypes.c_int), ("state_dtype", ctypes.c_int),
+                ("qk_norm", ctypes.c_int32), ("eps", ctypes.c_float), ("scale", ctypes.c_float)]
+
+
+class ConvDesc(ctypes.Structure):
+    _fields_ = [("batch", ctypes.c_int64), ("seqlen", ctypes.c_int64), ("dim", ctypes.c_int64),
+                ("width", ctypes.c_int64), ("x_stride", ctypes.c_int64),
+                ("in_dtype", ctypes.c_int), ("out_dtype", ctypes.c_int), ("silu", ctypes.c_int32)]
 
 
 _lib = None
@@ -113,6 +132,19 @@ def lib():
         L.precog_smc_consolidate.argtypes = [vp, ctypes.c_int, i64, i64, vp, ctypes.c_int, vp, i64,
                                              ctypes.c_double, vp]
         L.precog_smc_consolidate.restype = ctypes.c_int
+        L.precog_delta_encode.argtypes = [ctypes.POINTER(DeltaDesc)] + [vp] * 7 + [i64] + [vp] * 4
+        L.precog_delta_encode.restype = ctypes.c_int
+        L.precog_delta_step.argtypes = [ctypes.POINTER(DeltaDesc)] + [vp] * 6 + [i64] + [vp] * 3
+        L.precog_delta_step.restype = ctypes.c_int
+        L.precog_conv_encode.argtypes = [ctypes.POINTER(ConvDesc)] + [vp] * 5 + [i64] + [vp] * 4
+        L.precog_conv_encode.restype = ctypes.c_int
+        L.precog_conv_step.argtypes = [ctypes.POINTER(ConvDesc)] + [vp] * 4 + [i64] + [vp] * 3
+        L.precog_conv_step.restype = ctypes.c_int
+        L.precog_score_workspace_bytes.argtypes = [i64, i64, i64]
+        L.precog_score_workspace_bytes.restype = sz
+        L.precog_score_tokens.argtypes = [vp, ctypes.c_int, i64, i64, i64, vp, i64] + [vp] * 5 + \
+            [sz, vp]
+        L.precog_score_tokens.restype = ctypes.c_int
         L.precog_status_string.argtypes = [ctypes.c_int]
         L.precog_status_string.restype = ctypes.c_char_p
         _lib = L
@@ -348,6 +380,68 @@ def smc_consolidate(states, contrib, target, alpha, stream=None):
     _check("precog_smc_consolidate", st)
 
 
+def delta_desc(batch, seqlen, k_heads, v_heads, k_dim, v_dim, in_dtype=BF16, out_dtype=F32,
+               state_dtype=F32, q_stride=0, k_stride=0, v_stride=0, h0_batch_stride=0,
+               hT_batch_stride=0, qk_norm=False, eps=1e-6, scale=0.0) -> DeltaDesc:
+    return DeltaDesc(batch, seqlen, k_heads, v_heads, k_dim, v_dim, q_stride, k_stride, v_stride,
+                     h0_batch_stride, hT_batch_stride, in_dtype, out_dtype, state_dtype,
+                     1 if qk_norm else 0, eps, scale)
+
+
+def delta_encode(desc: DeltaDesc, q, k, v, g=None, beta=None, starts=None, h0=None, h0_rows=0,
+                 h0_idx=None, o=None, hT=None, stream=None):
+    """precog_delta_encode on device tensors (or raw device pointers)."""
+    st = lib().precog_delta_encode(ctypes.byref(desc), _ptr(q), _ptr(k), _ptr(v), _ptr(g),
+                                   _ptr(beta), _ptr(starts), _ptr(h0), int(h0_rows), _ptr(h0_idx),
+                                   _ptr(o), _ptr(hT), _stream(stream))
+    _check("precog_delta_encode", st)
+
+
+def delta_step_raw(desc: DeltaDesc, q, k, v, g, beta, states, state_rows, slots, o=None,
+                   stream=None):
+    """precog_delta_step on device tensors (or raw device pointers)."""
+    st = lib().precog_delta_step(ctypes.byref(desc), _ptr(q), _ptr(k), _ptr(v), _ptr(g),
+                                 _ptr(beta), _ptr(states), int(state_rows), _ptr(slots), _ptr(o),
+                                 _stream(stream))
+    _check("precog_delta_step", st)
+
+
+def conv_desc(batch, seqlen, dim, width, in_dtype=BF16, out_dtype=BF16, x_stride=0,
+              silu=True) -> ConvDesc:
+    return ConvDesc(batch, seqlen, dim, width, x_stride, in_dtype, out_dtype, 1 if silu else 0)
+
+
+def conv_encode(desc: ConvDesc, x, w, bias=None, starts=None, tail0=None, tail_rows=0,
+                tail_idx=None, y=None, tailT=None, stream=None):
+    """precog_conv_encode on device tensors (or raw device pointers)."""
+    st = lib().precog_conv_encode(ctypes.byref(desc), _ptr(x), _ptr(w), _ptr(bias), _ptr(starts),
+                                  _ptr(tail0), int(tail_rows), _ptr(tail_idx), _ptr(y),
+                                  _ptr(tailT), _stream(stream))
+    _check("precog_conv_encode", st)
+
+
+def conv_step_raw(desc: ConvDesc, x, w, bias, tails, tail_rows, slots, y=None, stream=None):
+    """precog_conv_step on device tensors (or raw device pointers)."""
+    st = lib().precog_conv_step(ctypes.byref(desc), _ptr(x), _ptr(w), _ptr(bias), _ptr(tails),
+                                int(tail_rows), _ptr(slots), _ptr(y), _stream(stream))
+    _check("precog_conv_step", st)
+
+
+def score_workspace_bytes(T, V, top) -> int:
+    return int(lib().precog_score_workspace_bytes(int(T), int(V), int(top)))
+
+
+def score_tokens_raw(logits, logits_dtype, T, V, row_stride, token, top, logprob, entropy=None,
+                     top_id=None, top_logprob=None, workspace=None, workspace_bytes=0,
+                     stream=None):
+    """precog_score_tokens on device tensors (or raw device pointers)."""
+    st = lib().precog_score_tokens(_ptr(logits), int(logits_dtype), int(T), int(V),
+                                   int(row_stride), _ptr(token), int(top), _ptr(logprob),
+                                   _ptr(entropy), _ptr(top_id), _ptr(top_logprob),
+                                   _ptr(workspace), int(workspace_bytes), _stream(stream))
+    _check("precog_score_tokens", st)
+
+
 # ----------------------------------------------------------------------------
 # Convenience wrappers that allocate outputs and workspace with torch.
 # ----------------------------------------------------------------------------
@@ -507,3 +601,244 @@ def gather(store, idx, out_dtype=None, stream=None):
                      device=store.device)
     inject_gather(store, idx, h0, stream)
     return h0
+
+
+# The gated-delta layer and token scoring.  These wrappers check what the
+# library cannot see (types, shapes, strides and devices of the tensors).
+def _same(name, t, dtype, shape, device, contiguous=True):
+    """t is a tensor of that type, shape and device (and contiguous), or a ValueError."""
+    if t.dtype != dtype or tuple(t.shape) != tuple(shape):
+        raise ValueError("%s must be %s %s, not %s %s" % (name, dtype, list(shape), t.dtype,
+                                                          list(t.shape)))
+    if t.device != device:
+        raise ValueError("%s is on %s, not on %s" % (name, t.device, device))
+    if contiguous and not t.is_contiguous():
+        raise ValueError("%s must be contiguous" % name)
+
+
+def _code(name, dtype, allowed):
+    if dtype not in allowed:
+        raise ValueError("%s must be one of %s, not %s" % (name, ", ".join(map(str, allowed)), dtype))
+    return _DT[dtype]
+
+
+_IO = (torch.float32, torch.bfloat16)
+_STATE = (torch.float32, torch.float16)
+
+
+def _device_of(t):
+    """t's device, which must be the current one: the library launches there."""
+    if not t.is_cuda:
+        raise ValueError("tensors must be on the GPU, not on %s" % t.device)
+    if t.device.index != torch.cuda.current_device():
+        raise ValueError("tensors are on %s but the current device is cuda:%d"
+                         % (t.device, torch.cuda.current_device()))
+    return t.device
+
+
+def _token_stride(name, t, lead):
+    """Elements between tokens of t, whose first `lead` axes are the tokens' (a
+    [B, L] batch, or one packed axis) and whose others are one token, which has
+    to be dense: a slice of a wider tensor's last axis is."""
+    inner = 1
+    for n, st in zip(reversed(t.shape[lead:]), reversed(t.stride()[lead:])):
+        if n != 1 and st != inner:
+            raise ValueError("%s: the elements of one token must be contiguous" % name)
+        inner *= n
+    if t.numel() == 0:
+        return 0
+    stride = t.stride(lead - 1) if t.shape[lead - 1] > 1 else 0
+    if lead == 2 and t.shape[0] > 1:
+        outer = t.stride(0)
+        if stride == 0:
+            stride = outer // t.shape[1]
+        if outer != stride * t.shape[1]:
+            raise ValueError("%s: the rows of a batch must follow one another" % name)
+    return 0 if stride == inner else stride
+
+
+class _Allocate:
+    """Outputs and workspace come from the stream that the kernels run on."""
+
+    def __init__(self, stream):
+        if isinstance(stream, int):
+            stream = torch.cuda.ExternalStream(stream)
+        self.scope = None if stream is None else torch.cuda.stream(stream)
+
+    def __enter__(self):
+        if self.scope is not None:
+            self.scope.__enter__()
+
+    def __exit__(self, *exc):
+        if self.scope is not None:
+            self.scope.__exit__(*exc)
+
+
+def _delta_args(q, k, v, g, beta, lead, out_dtype, state_dtype):
+    dev = _device_of(k)
+    if k.dim() != lead + 2 or v.dim() != lead + 2:
+        raise ValueError("k and v must have %d axes" % (lead + 2))
+    code = _code("k", k.dtype, _IO)
+    tokens, (Hk, K), (Hv, V) = k.shape[:lead], k.shape[lead:], v.shape[lead:]
+    if q is not None:
+        _same("q", q, k.dtype, k.shape, dev, contiguous=False)
+    _same("v", v, k.dtype, tuple(tokens) + (Hv, V), dev, contiguous=False)
+    for name, t in (("g", g), ("beta", beta)):
+        if t is not None:
+            _same(name, t, torch.float32, tuple(tokens) + (Hv,), dev)
+    strides = [0 if t is None else _token_stride(n, t, lead)
+               for n, t in (("q", q), ("k", k), ("v", v))]
+    return dev, (Hk, Hv, K, V), (code, _code("out_dtype", out_dtype, _IO),
+                                 _code("state_dtype", state_dtype, _STATE)), strides
+
+
+def delta(q, k, v, g=None, beta=None, h0=None, *, starts=None, h0_idx=None, qk_norm=False,
+          eps=1e-6, scale=0.0, out_dtype=torch.float32, state_dtype=None, want_o=True,
+          want_hT=True, hT=None, stream=None):
+    """The gated delta rule over whole sequences; returns (o, hT) (None where
+    not wanted).
+
+    q, k [B, L, Hk, K] and v [B, L, Hv, V], or with starts [B + 1] (int32) the
+    packed [T, Hk, K] and [T, Hv, V]; g (log decay) and beta [..., Hv] fp32;
+    h0 [B, Hv, K, V] or, with h0_idx [B] int32, a store [rows, Hv, K, V] whose
+    rows h0_idx names the sequences start from.  q None with want_o False: the
+    states only.  hT: a tensor for the states (h0 itself: in place)."""
+    lead = 2 if starts is None else 1
+    if q is None and want_o:
+        raise ValueError("o needs q")
+    state_dtype = state_dtype or (h0.dtype if h0 is not None else torch.float32)
+    dev, (Hk, Hv, K, V), codes, strides = _delta_args(q, k, v, g, beta, lead, out_dtype,
+                                                      state_dtype)
+    if starts is not None:
+        if starts.dim() != 1 or starts.shape[0] < 1:
+            raise ValueError("starts must have B + 1 entries")
+        _same("starts", starts, torch.int32, starts.shape, dev)
+        B, L = starts.shape[0] - 1, k.shape[0]
+    else:
+        B, L = k.shape[0], k.shape[1]
+    if h0_idx is not None:
+        _same("h0_idx", h0_idx, torch.int32, (B,), dev)
+        if h0 is None:
+            raise ValueError("h0_idx needs a store h0")
+    if h0 is not None:
+        rows = h0.shape[0] if h0_idx is not None else B
+        _same("h0", h0, state_dtype, (rows, Hv, K, V), dev)
+    if hT is not None:
+        _same("hT", hT, state_dtype, (B, Hv, K, V), dev)
+    desc = delta_desc(B, L, Hk, Hv, K, V, *codes, *strides, 0, 0, qk_norm, eps, scale)
+    with _Allocate(stream):
+        o = torch.empty(tuple(v.shape), dtype=out_dtype, device=dev) if want_o else None
+        if want_hT and hT is None:
+            hT = torch.empty((B, Hv, K, V), dtype=state_dtype, device=dev)
+    delta_encode(desc, q, k, v, g, beta, starts, h0, h0.shape[0] if h0 is not None else 0, h0_idx,
+                 o, hT, stream)
+    return o, hT
+
+
+def delta_step(q, k, v, g, beta, states, slots, *, qk_norm=False, eps=1e-6, scale=0.0,
+               out_dtype=torch.float32, want_o=True, stream=None):
+    """One token of each of n sessions: q, k [n, Hk, K], v [n, Hv, V], g and
+    beta [n, Hv] fp32 or None; row i's state is states[slots[i]] (states
+    [rows, Hv, K, V], slots int32), updated in place.  Returns o [n, Hv, V]; the
+    rows of o whose slot is outside the states are not written."""
+    dev, (Hk, Hv, K, V), codes, strides = _delta_args(q, k, v, g, beta, 1, out_dtype, states.dtype)
+    if q is None and want_o:
+        raise ValueError("o needs q")
+    n = k.shape[0]
+    _same("states", states, states.dtype, (states.shape[0], Hv, K, V), dev)
+    _same("slots", slots, torch.int32, (n,), dev)
+    desc = delta_desc(n, 1, Hk, Hv, K, V, *codes, *strides, 0, 0, qk_norm, eps, scale)
+    with _Allocate(stream):
+        o = torch.empty((n, Hv, V), dtype=out_dtype, device=dev) if want_o else None
+    delta_step_raw(desc, q, k, v, g, beta, states, states.shape[0], slots, o, stream)
+    return o
+
+
+def _conv_args(x, w, bias, lead, out_dtype):
+    dev = _device_of(x)
+    if x.dim() != lead + 1 or w.dim() != 2:
+        raise ValueError("x must have %d axes and w two" % (lead + 1))
+    D, W = x.shape[-1], w.shape[1]
+    _same("w", w, torch.float32, (D, W), dev)
+    if bias is not None:
+        _same("bias", bias, torch.float32, (D,), dev)
+    return dev, D, W, (_code("x", x.dtype, _IO), _code("out_dtype", out_dtype, _IO)), \
+        _token_stride("x", x, lead)
+
+
+def conv(x, w, bias=None, tail0=None, *, starts=None, tail_idx=None, silu=True, out_dtype=None,
+         want_y=True, want_tail=True, tailT=None, stream=None):
+    """The short causal convolution; returns (y, tailT).  x [B, L, D], or with
+    starts [B + 1] (int32) the packed [T, D]; w [D, W] and bias [D] fp32; tail0
+    [B, W - 1, D], or with tail_idx [B] int32 a store of tails.  tailT: a tensor
+    for the tails (tail0 itself: in place)."""
+    lead = 2 if starts is None else 1
+    out_dtype = out_dtype or x.dtype
+    dev, D, W, codes, stride = _conv_args(x, w, bias, lead, out_dtype)
+    if starts is not None:
+        if starts.dim() != 1 or starts.shape[0] < 1:
+            raise ValueError("starts must have B + 1 entries")
+        _same("starts", starts, torch.int32, starts.shape, dev)
+        B, L = starts.shape[0] - 1, x.shape[0]
+    else:
+        B, L = x.shape[0], x.shape[1]
+    if tail_idx is not None:
+        _same("tail_idx", tail_idx, torch.int32, (B,), dev)
+        if tail0 is None:
+            raise ValueError("tail_idx needs a store tail0")
+    if tail0 is not None:
+        rows = tail0.shape[0] if tail_idx is not None else B
+        _same("tail0", tail0, x.dtype, (rows, W - 1, D), dev)
+    if tailT is not None:
+        _same("tailT", tailT, x.dtype, (B, W - 1, D), dev)
+    desc = conv_desc(B, L, D, W, *codes, stride, silu)
+    with _Allocate(stream):
+        y = torch.empty(tuple(x.shape), dtype=out_dtype, device=dev) if want_y else None
+        if want_tail and tailT is None:
+            tailT = torch.empty((B, max(W - 1, 0), D), dtype=x.dtype, device=dev)
+    conv_encode(desc, x, w, bias, starts, tail0, tail0.shape[0] if tail0 is not None else 0,
+                tail_idx, y, tailT, stream)
+    return y, tailT
+
+
+def conv_step(x, w, bias, tails, slots, *, silu=True, out_dtype=None, stream=None):
+    """One token of each of n sessions: x [n, D]; row i's tail is tails[slots[i]]
+    (tails [rows, W - 1, D], slots int32), moved on in place.  Returns y [n, D];
+    the rows of y whose slot is outside the tails are not written."""
+    out_dtype = out_dtype or x.dtype
+    dev, D, W, codes, stride = _conv_args(x, w, bias, 1, out_dtype)
+    n = x.shape[0]
+    _same("tails", tails, x.dtype, (tails.shape[0], W - 1, D), dev)
+    _same("slots", slots, torch.int32, (n,), dev)
+    desc = conv_desc(n, 1, D, W, *codes, stride, silu)
+    with _Allocate(stream):
+        y = torch.empty((n, D), dtype=out_dtype, device=dev)
+    conv_step_raw(desc, x, w, bias, tails, tails.shape[0], slots, y, stream)
+    return y
+
+
+def score_tokens(logits, token=None, top=0, *, want_entropy=True, stream=None):
+    """Log probabilities of token [T] (int32) under logits [T, V] (fp32, bf16 or
+    fp16; rows may be strided), with the entropies and the `top` alternatives:
+    (logprob [T], entropy [T], top_id [T, top], top_logprob [T, top]), None where
+    not wanted."""
+    dev = _device_of(logits)
+    if logits.dim() != 2:
+        raise ValueError("logits must be [T, V]")
+    T, V = logits.shape
+    code = _code("logits", logits.dtype, (torch.float32, torch.bfloat16, torch.float16))
+    if V > 1 and logits.stride(1) != 1:
+        raise ValueError("logits: the elements of a row must be contiguous")
+    stride = logits.stride(0) if T > 1 else V
+    if token is not None:
+        _same("token", token, torch.int32, (T,), dev)
+    nbytes = score_workspace_bytes(T, V, top)
+    with _Allocate(stream):
+        logprob = torch.empty(T, dtype=torch.float32, device=dev) if token is not None else None
+        entropy = torch.empty(T, dtype=torch.float32, device=dev) if want_entropy else None
+        top_id = torch.empty((T, top), dtype=torch.int32, device=dev) if top else None
+        top_logprob = torch.empty((T, top), dtype=torch.float32, device=dev) if top else None
+        ws = torch.empty(nbytes, dtype=torch.uint8, device=dev) if nbytes else None
+    score_tokens_raw(logits, code, T, V, stride, token, top, logprob, entropy, top_id, top_logprob,
+                     ws, nbytes, stream)
+    return logprob, entropy, top_id, top_logprob

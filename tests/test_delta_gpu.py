@@ -1,0 +1,357 @@
+"""The gated delta rule on the GPU against the sequential fp64 oracle: whole
+sequences (packed and padded batches, injected and captured states) and single
+tokens of running sessions."""
+import numpy as np
+import pytest
+import torch
+
+import oracle
+from layer_testutil import check, delta_bar, delta_inputs, delta_oracle, on_gpu, starts_of
+from paper_2608_02560_amd import precog as P
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda"
+
+
+def _states(rows, Hv, K, V, dtype, seed):
+    gen = torch.Generator().manual_seed(seed)
+    return (torch.randn((rows, Hv, K, V), generator=gen) * 0.5).to(dtype)
+
+
+def _run(lens, Hk, Hv, K, V, dtype=torch.bfloat16, out=torch.float32, st=torch.float32, norm=True, seed=1, h0=True,
+         **kw):
+    d = delta_inputs(sum(lens), Hk, Hv, K, V, seed, dtype, unit=not norm, **kw)
+    S0 = _states(len(lens), Hv, K, V, st, seed + 1) if h0 else None
+    c = on_gpu(d)
+    o, hT = P.delta(c["q"], c["k"], c["v"], c["g"], c["beta"], None if S0 is None else S0.to(DEV),
+                    starts=starts_of(lens).to(DEV), qk_norm=norm, out_dtype=out, state_dtype=st)
+    ro, rS = delta_oracle(d, lens, S0, qk_norm=norm)
+    bar = delta_bar(max(lens))
+    check(o, ro, bar, "o")
+    check(hT, rS, bar, "hT")
+
+
+@pytest.mark.parametrize("K,V", [(128, 128), (64, 64), (96, 80), (8, 8), (64, 256), (128, 24), (40, 136)])
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+def test_head_sizes(K, V, dtype):
+    _run([33, 7], 1, 2, K, V, dtype, norm=dtype == torch.bfloat16)
+
+
+@pytest.mark.parametrize("lens", [[1], [2, 1, 3], [31], [32], [33], [63, 64, 65], [0, 5, 0, 0, 40, 0], [300],
+                                  [129, 1, 600]])
+@pytest.mark.parametrize("K,V", [(128, 128), (64, 48)])
+def test_lengths(lens, K, V):
+    _run(lens, 1, 1, K, V)
+
+
+@pytest.mark.parametrize("Hk,Hv", [(1, 1), (1, 3), (2, 4), (3, 3), (2, 10)])
+def test_heads(Hk, Hv):
+    _run([37, 64], Hk, Hv, 64, 64)
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("out", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("st", [torch.float16, torch.float32])
+@pytest.mark.parametrize("norm", [True, False])
+def test_types(dtype, out, st, norm):
+    _run([70, 20], 1, 2, 128, 64, dtype, out, st, norm)
+
+
+@pytest.mark.parametrize("h0", [True, False])
+def test_contiguous_inputs(h0):
+    _run([50], 2, 2, 64, 64, h0=h0, sliced=False)
+
+
+def test_many_workgroups():
+    """More heads than CUs: the wide column split."""
+    _run([40] * 70, 4, 16, 64, 128, torch.bfloat16, torch.bfloat16, torch.float16)
+
+
+def test_padded_batch_equals_packed():
+    B, L, Hk, Hv, K, V = 3, 45, 2, 4, 64, 64
+    d = on_gpu(delta_inputs(B * L, Hk, Hv, K, V, 5))
+    packed = P.delta(d["q"], d["k"], d["v"], d["g"], d["beta"], starts=starts_of([L] * B).to(DEV), qk_norm=True)
+    r = {n: t.unflatten(0, (B, L)) for n, t in d.items()}
+    batch = P.delta(r["q"], r["k"], r["v"], r["g"], r["beta"], qk_norm=True)
+    assert torch.equal(packed[0].view(batch[0].shape), batch[0])
+    assert torch.equal(packed[1], batch[1])
+
+
+def test_absent_gates_and_scale():
+    d = delta_inputs(50, 1, 2, 64, 64, 6, unit=True)
+    c = on_gpu(d)
+    o, hT = P.delta(c["q"], c["k"], c["v"], starts=starts_of([50]).to(DEV), scale=0.75)
+    ro, rS = delta_oracle(dict(d, g=None, beta=None), [50], scale=0.75)
+    check(o, ro, delta_bar(50))
+    check(hT, rS, delta_bar(50))
+
+
+def test_states_only_equals_the_full_call():
+    d = on_gpu(delta_inputs(90, 2, 4, 128, 128, 7))
+    starts = starts_of([90]).to(DEV)
+    _, hT = P.delta(d["q"], d["k"], d["v"], d["g"], d["beta"], starts=starts, qk_norm=True)
+    o, only = P.delta(None, d["k"], d["v"], d["g"], d["beta"], starts=starts, qk_norm=True, want_o=False)
+    assert o is None and torch.equal(hT, only)
+
+
+@pytest.mark.parametrize("st", [torch.float32, torch.float16])
+def test_injection_from_a_store(st):
+    lens, rows = [5, 40, 0, 33, 1], 9
+    d = delta_inputs(sum(lens), 2, 4, 64, 64, 8)
+    store = _states(rows, 4, 64, 64, st, 9)
+    idx = torch.tensor([3, 8, 0, 3, 9], dtype=torch.int32)  # the last names no row
+    c = on_gpu(d)
+    o, hT = P.delta(c["q"], c["k"], c["v"], c["g"], c["beta"], store.to(DEV), starts=starts_of(lens).to(DEV),
+                    h0_idx=idx.to(DEV), qk_norm=True)
+    h0 = store[idx.clamp(max=rows - 1).long()].clone()
+    ro, rS = delta_oracle(d, lens, h0, qk_norm=True)
+    n = sum(lens[:4])
+    check(o[:n], ro[:n], delta_bar(40))
+    check(hT[:4], rS[:4], delta_bar(40))
+    assert torch.isnan(o[n:]).all() and torch.isnan(hT[4]).all()
+
+
+def test_a_split_continues_the_sequence():
+    """S(h0, c ++ q) = S(S(h0, c), q), with the state passed in 32 bits, in place."""
+    d = delta_inputs(140, 1, 2, 128, 128, 10)
+    c = on_gpu(d)
+    state = torch.zeros((1, 2, 128, 128), device=DEV)
+    outs = []
+    for a, b in ((0, 61), (61, 62), (62, 140)):
+        p = {n: t[a:b] for n, t in c.items()}
+        o, hT = P.delta(p["q"], p["k"], p["v"], p["g"], p["beta"], state,
+                        starts=starts_of([b - a]).to(DEV), qk_norm=True, hT=state)
+        assert hT is state
+        outs.append(o)
+    ro, rS = delta_oracle(d, [140], qk_norm=True)
+    check(torch.cat(outs), ro, delta_bar(140))
+    check(state, rS, delta_bar(140))
+
+
+def test_layers_of_one_store():
+    """States written into a layer's slots of a multi-layer store."""
+    B, Hv, K, V, layers = 3, 2, 64, 64, 4
+    d = delta_inputs(B * 20, 2, Hv, K, V, 11)
+    c = on_gpu(d)
+    sd = Hv * K * V
+    store = torch.full((B, layers, Hv, K, V), 7.0, device=DEV, dtype=torch.float16)
+    store[:, 1] = _states(B, Hv, K, V, torch.float16, 12).to(DEV)
+    before = store.clone()
+    desc = P.delta_desc(B, 20, 2, Hv, K, V, P.BF16, P.F32, P.F16, *[c[n].stride(0) for n in ("q", "k", "v")],
+                        layers * sd, layers * sd, True)
+    P.delta_encode(desc, c["q"], c["k"], c["v"], c["g"], c["beta"], None, store[:, 1].data_ptr(), B, None, None,
+                   store[:, 2].data_ptr())
+    _, rS = delta_oracle(dict(d, q=None), [20] * B, before[:, 1].cpu(), qk_norm=True)
+    check(store[:, 2], rS, delta_bar(20))
+    for l in (0, 1, 3):
+        assert torch.equal(store[:, l], before[:, l])
+
+
+def test_rows_outside_the_sequences_stay():
+    T = 60
+    d = on_gpu(delta_inputs(T, 1, 1, 64, 64, 13))
+    starts = torch.tensor([4, 20, 20, 51], dtype=torch.int32, device=DEV)
+    o = torch.full((T, 1, 64), 3.5, device=DEV)
+    hT = torch.empty((3, 1, 64, 64), device=DEV)
+    desc = P.delta_desc(3, T, 1, 1, 64, 64, qk_norm=True, q_stride=d["q"].stride(0), k_stride=d["k"].stride(0),
+                        v_stride=d["v"].stride(0))
+    P.delta_encode(desc, d["q"], d["k"], d["v"], d["g"], d["beta"], starts, o=o, hT=hT)
+    assert (o[:4] == 3.5).all() and (o[51:] == 3.5).all() and not (o[4:51] == 3.5).any()
+    assert (hT[1] == 0).all()
+
+
+def test_bad_starts_are_clamped():
+    T = 40
+    d = on_gpu(delta_inputs(T, 1, 1, 64, 64, 14))
+    good = P.delta(d["q"], d["k"], d["v"], d["g"], d["beta"], starts=starts_of([10, 30]).to(DEV), qk_norm=True)
+    starts = torch.tensor([-5, 10, 1 << 30], dtype=torch.int32, device=DEV)
+    bad = P.delta(d["q"], d["k"], d["v"], d["g"], d["beta"], starts=starts, qk_norm=True)
+    assert torch.equal(good[0], bad[0]) and torch.equal(good[1], bad[1])
+    starts = torch.tensor([30, 10, 40], dtype=torch.int32, device=DEV)  # ends before it begins: empty
+    o, hT = P.delta(d["q"], d["k"], d["v"], d["g"], d["beta"], starts=starts, qk_norm=True)
+    assert torch.equal(o[10:], good[0][10:]) and (hT[0] == 0).all() and torch.equal(hT[1], good[1][1])
+
+
+def test_strong_decays():
+    """Log decays that empty the state, -infinity and far below fp32 among them."""
+    d = delta_inputs(100, 1, 2, 64, 64, 15)
+    d["g"][10] = -np.inf
+    d["g"][40, 0] = -1e30
+    d["g"][41:60, 1] = -30.0
+    d["g"][99] = -300.0
+    c = on_gpu(d)
+    o, hT = P.delta(c["q"], c["k"], c["v"], c["g"], c["beta"], starts=starts_of([100]).to(DEV), qk_norm=True)
+    ro, rS = delta_oracle(d, [100], qk_norm=True)
+    check(o, ro, delta_bar(100))
+    check(hT, rS, delta_bar(100))
+
+
+@pytest.mark.parametrize("beta", [0.0, 1.0])
+def test_repeated_keys(beta):
+    """One key throughout: with beta 1 and no decay the state answers it with the last value."""
+    d = delta_inputs(80, 1, 1, 128, 64, 16)
+    d["k"][:] = d["k"][0].clone()
+    d["q"][:] = d["k"]
+    d["beta"][:] = beta
+    c = on_gpu(d)
+    o, hT = P.delta(c["q"], c["k"], c["v"], None, c["beta"], starts=starts_of([80]).to(DEV), qk_norm=True)
+    ro, rS = delta_oracle(dict(d, g=None), [80], qk_norm=True)
+    check(o, ro, delta_bar(80))
+    check(hT, rS, delta_bar(80))
+
+
+@pytest.mark.parametrize("size", [1e-12, 1e-3, 1e4, 1e15])
+def test_value_and_key_magnitudes(size):
+    """Values far from one scale o and the states; keys' sizes fall out with the norm."""
+    d = delta_inputs(70, 1, 1, 64, 64, 17, torch.float32)
+    d["v"] = (d["v"] * size).contiguous()
+    d["k"] = (d["k"] * min(max(size, 0.5), 1e3)).contiguous()
+    d["q"] = d["q"].contiguous()
+    c = on_gpu(d)
+    o, hT = P.delta(c["q"], c["k"], c["v"], c["g"], c["beta"], starts=starts_of([70]).to(DEV), qk_norm=True)
+    ro, rS = delta_oracle(d, [70], qk_norm=True)
+    check(o, ro, delta_bar(70))
+    check(hT, rS, delta_bar(70))
+
+
+def test_zero_keys_and_values():
+    d = delta_inputs(50, 1, 1, 64, 64, 18)
+    d["k"][5:20] = 0
+    d["q"][7] = 0
+    d["v"][30:] = 0
+    c = on_gpu(d)
+    o, hT = P.delta(c["q"], c["k"], c["v"], c["g"], c["beta"], starts=starts_of([50]).to(DEV), qk_norm=True)
+    ro, rS = delta_oracle(d, [50], qk_norm=True)
+    check(o, ro, delta_bar(50))
+    check(hT, rS, delta_bar(50))
+
+
+def test_non_finite_tokens_stay_in_their_sequence_and_head():
+    d = delta_inputs(160, 2, 2, 64, 64, 19)
+    lens = [80, 80]
+    clean = {n: t.clone() for n, t in d.items()}
+    d["v"][40, 1, 3] = float("nan")
+    d["g"][120, 0] = float("nan")
+    c, s = on_gpu(d), starts_of(lens).to(DEV)
+    o, hT = P.delta(c["q"], c["k"], c["v"], c["g"], c["beta"], starts=s, qk_norm=True)
+    c = on_gpu(clean)
+    ro, rT = P.delta(c["q"], c["k"], c["v"], c["g"], c["beta"], starts=s, qk_norm=True)
+    assert torch.isnan(hT[0, 1]).any() and torch.isnan(hT[1, 0]).any()
+    assert torch.equal(hT[0, 0], rT[0, 0]) and torch.equal(hT[1, 1], rT[1, 1])
+    assert torch.equal(o[:80, 0], ro[:80, 0]) and torch.equal(o[80:, 1], ro[80:, 1])
+    assert torch.equal(o[:32, 1], ro[:32, 1]) and torch.equal(o[80:112, 0], ro[80:112, 0])
+    assert torch.isnan(o[40:80, 1]).any(-1).all() and torch.isnan(o[120:, 0]).any(-1).all()
+
+
+def test_long_sequence():
+    _run([2500], 1, 1, 64, 32, torch.bfloat16, torch.bfloat16, torch.float32)
+
+
+def test_two_runs_are_bitwise_equal():
+    d = on_gpu(delta_inputs(400, 2, 4, 128, 128, 20))
+    s = starts_of([150, 250]).to(DEV)
+    a = P.delta(d["q"], d["k"], d["v"], d["g"], d["beta"], starts=s, qk_norm=True)
+    b = P.delta(d["q"], d["k"], d["v"], d["g"], d["beta"], starts=s, qk_norm=True)
+    assert torch.equal(a[0], b[0]) and torch.equal(a[1], b[1])
+
+
+# ---------------------------------------------------------------- single tokens
+def _step_oracle(d, states, slots, st, **kw):
+    S = states.double().numpy().copy()
+    o = np.full((len(slots),) + tuple(d["v"].shape[1:]), np.nan)
+    for i, s in enumerate(slots):
+        if not 0 <= s < S.shape[0]:
+            continue
+        one = {n: None if t is None else t[i:i + 1] for n, t in d.items()}
+        o[i:i + 1], S[s] = oracle.delta(one["q"], one["k"], one["v"], one["g"], one["beta"], S[s], **kw)
+        if st == torch.float16:
+            S[s] = oracle.round_f16(S[s])
+    return o, S
+
+
+@pytest.mark.parametrize("n", [1, 5, 90])
+@pytest.mark.parametrize("K,V", [(128, 128), (64, 64), (96, 40), (8, 256)])
+def test_step_sizes(n, K, V):
+    rows, Hk, Hv = n + 3, 2, 4
+    d = delta_inputs(n, Hk, Hv, K, V, 30 + n)
+    states = _states(rows, Hv, K, V, torch.float32, 31)
+    slots = np.random.default_rng(n).permutation(rows)[:n].astype(np.int32)
+    c, s = on_gpu(d), states.to(DEV)
+    o = P.delta_step(c["q"], c["k"], c["v"], c["g"], c["beta"], s, torch.tensor(slots, device=DEV), qk_norm=True)
+    ro, rS = _step_oracle(d, states, slots, torch.float32, qk_norm=True)
+    check(o, ro, delta_bar(1))
+    check(s, rS, delta_bar(1))
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("out", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("st", [torch.float16, torch.float32])
+def test_step_types_and_odd_slots(dtype, out, st):
+    """Slots outside the states leave everything, repeated ones apply in order."""
+    slots = np.array([4, -1, 2, 4, 99, 0, 4, 2], dtype=np.int32)
+    n, Hv, K, V = len(slots), 2, 64, 96
+    d = delta_inputs(n, 1, Hv, K, V, 40, dtype, unit=True)
+    states = _states(6, Hv, K, V, st, 41)
+    c, s = on_gpu(d), states.to(DEV)
+    o = torch.full((n, Hv, V), 2.5, dtype=out, device=DEV)
+    desc = P.delta_desc(n, 1, 1, Hv, K, V, P._DT[dtype], P._DT[out], P._DT[st],
+                        *[c[x].stride(0) for x in ("q", "k", "v")])
+    P.delta_step_raw(desc, c["q"], c["k"], c["v"], c["g"], c["beta"], s, 6, torch.tensor(slots, device=DEV), o)
+    ro, rS = _step_oracle(d, states, slots, st)
+    live = (slots >= 0) & (slots < 6)
+    # A 16-bit state element of an earlier token that lies within the fp32 error
+    # of the middle of a step may be rounded the other way than the oracle's: a
+    # step of 2^-10 |S_ij|.  Such a state is off by that, and o_j by scale |q_i|
+    # 2^-10 |S_ij|; with |S_ij| up to 4 rms(S), |q_i| up to 4 / sqrt(K) = 1/2 for
+    # a unit q, and rms(o) = scale rms(S), that is 2^-9 rms(o) an element, 2^-8
+    # with a few of them in one sum.
+    flip = st == torch.float16
+    check(o[torch.tensor(live)], ro[live], delta_bar(4) + (2.0 ** -8 if flip else 0))
+    assert (o[torch.tensor(~live)] == 2.5).all()
+    check(s, rS, delta_bar(4) + (2.0 ** -10 if flip else 0))
+    for r in (1, 3, 5):
+        assert torch.equal(s[r].cpu(), states[r])
+
+
+def test_step_repeated_slots_equal_separate_calls():
+    n, Hv, K, V = 6, 2, 64, 64
+    d = on_gpu(delta_inputs(n, 2, Hv, K, V, 42))
+    for st in (torch.float16, torch.float32):
+        one = _states(2, Hv, K, V, st, 43).to(DEV)
+        two = one.clone()
+        slots = torch.tensor([1, 0, 1, 1, 0, 1], dtype=torch.int32, device=DEV)
+        a = P.delta_step(d["q"], d["k"], d["v"], d["g"], d["beta"], one, slots, qk_norm=True)
+        for i in range(n):
+            b = P.delta_step(d["q"][i:i + 1], d["k"][i:i + 1], d["v"][i:i + 1], d["g"][i:i + 1], d["beta"][i:i + 1],
+                             two, slots[i:i + 1].clone(), qk_norm=True)
+            assert torch.equal(a[i], b[0])
+        assert torch.equal(one, two)
+
+
+def test_step_continues_the_prefill():
+    """A prefill and then single tokens equal the whole sequence."""
+    lens, T = [30, 12, 41], 7
+    full = [delta_inputs(n + T, 2, 4, 128, 64, 50 + i) for i, n in enumerate(lens)]
+    pre = on_gpu({x: torch.cat([f[x][:n] for f, n in zip(full, lens)]) for x in full[0]})
+    states = torch.zeros((5, 4, 128, 64), device=DEV)
+    slots = torch.tensor([3, 0, 4], dtype=torch.int32, device=DEV)
+    _, hT = P.delta(pre["q"], pre["k"], pre["v"], pre["g"], pre["beta"], starts=starts_of(lens).to(DEV), qk_norm=True)
+    states[slots.long()] = hT
+    for t in range(T):
+        tok = on_gpu({x: torch.stack([f[x][n + t] for f, n in zip(full, lens)]) for x in full[0]})
+        o = P.delta_step(tok["q"], tok["k"], tok["v"], tok["g"], tok["beta"], states, slots, qk_norm=True)
+    for i, f in enumerate(full):
+        ro, rS = oracle.delta(f["q"], f["k"], f["v"], f["g"], f["beta"], qk_norm=True)
+        check(o[i], ro[-1], delta_bar(lens[i] + T))
+        check(states[slots[i].long()], rS, delta_bar(lens[i] + T))
+    assert (states[1] == 0).all() and (states[2] == 0).all()
+
+
+def test_step_without_outputs_and_gates():
+    d = delta_inputs(3, 1, 1, 64, 64, 60, unit=True)
+    states = _states(3, 1, 64, 64, torch.float32, 61)
+    c, s = on_gpu(d), states.to(DEV)
+    slots = torch.tensor([2, 1, 0], dtype=torch.int32, device=DEV)
+    assert P.delta_step(None, c["k"], c["v"], None, None, s, slots, want_o=False) is None
+    _, rS = _step_oracle(dict(d, g=None, beta=None), states, [2, 1, 0], torch.float32)
+    check(s, rS, delta_bar(1))
