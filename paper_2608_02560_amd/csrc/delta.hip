@@ -1,0 +1,894 @@
+// The gated delta rule over whole sequences, a block of 32 tokens at a time.
+//
+// With b_i the sum of the log decays of a block's tokens up to i, G_ij =
+// exp(b_i - b_j) for i >= j, S the state before the block and u_i the values
+// that the tokens write:
+//
+//   A_ij = beta_i G_ij k_i.k_j  (i > j),   T = (I + A)^-1 diag(beta)
+//   X = V - diag(e^b) K S,   U = T X
+//   O = scale (diag(e^b) Q S + (G . Q K^T) U)
+//   S <- e^{b_end} S + K^T diag(e^{b_end - b}) U
+//
+// so a block is a handful of small matrix products, and only those with S
+// depend on the block before.  One workgroup owns one head of one sequence (or
+// some of its columns: the columns of S and V do not meet).  Two kinds of
+// waves share it:
+//
+//   prepare  one wave takes a block from the queries, keys and gates to the
+//            matrix operands K, K^T, Q, T, G . QK^T and the row factors, in
+//            LDS, some blocks ahead of their use;
+//   chain    each wave keeps its columns of S in registers and runs the
+//            dependent products; no operand of it that changes leaves the
+//            wave, since a product's result lies in the registers as the next
+//            product wants its operand.
+//
+// Operands.  v_mfma_f32_16x16x32_f16 takes rows (columns) l % 16 and the eight
+// depths 8 (l / 16) + j of its operands from lane l, and gives lane l the rows
+// 4 (l / 16) + r of column l % 16.  Two results of 16 rows are therefore one
+// operand of depth 32 whose depth 8 q + j is row 4 q + j of the first (j < 4)
+// or row 4 q + j - 4 of the second, and the other operand is laid out to match.
+//
+// Numbers.  The states, all sums, decays and norms are fp32 (b is summed in
+// fp64, where the differences of two positions are taken).  A product's
+// operands are fp16: keys and queries as 2^e times unit size (exact for bf16
+// up to 2^-30 of the row's norm; fp32 inputs as two halves of 11 bits), and S,
+// X, U and T as two halves (22 bits) under a power of two that puts their
+// column's (T: block's) largest at 2^14, so neither half runs out of range.
+// Products of two low halves are left out (2^-22).  What only enters a bf16 o
+// (Q S, Q K^T U) takes the high halves alone: 2^-11 against the 2^-8 of o.
+#include "layer_ops.h"
+#include "wave_ops.h"
+
+namespace precog {
+namespace {
+
+constexpr int kBlockTokens = 32;
+constexpr int kChainMax = 4;     // chain waves of a workgroup
+constexpr int kAStride = 36;     // floats between rows of A in LDS: 16-byte rows on shifting banks
+constexpr float kLog2e = 1.44269504088896341f;
+
+typedef _Float16 half8 __attribute__((ext_vector_type(8)));
+typedef _Float16 half4 __attribute__((ext_vector_type(4)));
+typedef _Float16 half2 __attribute__((ext_vector_type(2)));
+typedef float float2v __attribute__((ext_vector_type(2)));
+typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+typedef float float4v __attribute__((ext_vector_type(4)));
+typedef uint32_t uint2v __attribute__((ext_vector_type(2)));
+typedef uint32_t uint4v __attribute__((ext_vector_type(4)));
+
+// Row factors of a block's tokens, and what belongs to the block.
+struct Factors {
+  float x[kBlockTokens];   // e^b |k| of X's subtrahend
+  float r[kBlockTokens];   // |k| of a row of U before Q K^T
+  float u[kBlockTokens];   // e^{b_end - b} |k| of a row of U before K^T
+  float q[kBlockTokens];   // scale |q| e^b of Q S
+  float o[kBlockTokens];   // scale |q| of Q K^T U
+  float decay;             // e^{b_end}
+  float t;                 // power of two that T's operand lacks
+  float most;              // largest of r and u
+  float pad;
+};
+
+// A block's operands in LDS, in 1 KB fragments of one matrix instruction.
+template <int KP, bool IN32, bool OUT32>
+struct Buffer {
+  static constexpr int kHalves = IN32 ? 2 : 1;
+  static constexpr int kSteps = KP / 32;
+  half8 k[kHalves][2][kSteps][64];    // token tile, depth step
+  half8 q[kHalves][2][kSteps][64];
+  half8 kt[kHalves][KP / 16][64];     // state row tile; depth: the block's tokens
+  half8 t[2][2][64];                  // half, token tile
+  half8 p[OUT32 ? 2 : 1][2][64];
+  Factors f;
+};
+
+// A prepare wave's own LDS.
+struct Scratch {
+  float a[kBlockTokens * kAStride];
+  double b[kBlockTokens];
+  float rk[kBlockTokens];
+  float rq[kBlockTokens];
+  float beta[kBlockTokens];
+};
+
+template <int KP, bool IN32, bool OUT32>
+struct Shared {
+  static constexpr int kBuffers = IN32 ? 2 : 4;   // as many as fit into 160 KB
+  static constexpr int kPrepare = kBuffers - 1;   // prepare waves: each works on a buffer of its own
+  Buffer<KP, IN32, OUT32> buf[kBuffers];
+  Scratch scratch[kPrepare];
+  int ready[kBuffers];       // block held by the buffer, counted from 1
+  int done[kChainMax];       // blocks that the chain wave has read
+};
+
+__device__ __forceinline__ float4v mfma(half8 a, half8 b, float4v c) {
+  return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0);
+}
+__device__ __forceinline__ float4v mfma(float a, float b, float4v c) {
+  return __builtin_amdgcn_mfma_f32_16x16x4f32(a, b, c, 0, 0, 0);
+}
+
+__device__ __forceinline__ half2 to_half2(float a, float b) {
+  return __builtin_convertvector((float2v{a, b}), half2);  // nearest even
+}
+
+// Orders a wave's LDS accesses before and after it (other lanes' among them).
+__device__ __forceinline__ void wave_fence() {
+  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+  __builtin_amdgcn_wave_barrier();
+}
+
+__device__ __forceinline__ float max_abs(float m, float v) { return fmaxf(m, fabsf(v)); }
+
+// The largest of lanes l, l ^ 16, l ^ 32 and l ^ 48.
+__device__ __forceinline__ float max_of_rows(float v) {
+  const uint32_t b = __float_as_uint(v);
+  const auto s = __builtin_amdgcn_permlane32_swap(b, b, false, false);
+  const float m = fmaxf(__uint_as_float(s[0]), __uint_as_float(s[1]));
+  const uint32_t c = __float_as_uint(m);
+  const auto t = __builtin_amdgcn_permlane16_swap(c, c, false, false);
+  return fmaxf(__uint_as_float(t[0]), __uint_as_float(t[1]));
+}
+
+// 2^e and 2^-e with 2^e m in [2^14, 2^15), e bounded where one of them would
+// leave fp32.
+struct Scale {
+  float up, down;
+};
+__device__ __forceinline__ Scale scale_of(float m) {
+  int e = static_cast<int>(__float_as_uint(m) >> 23 & 255);
+  e = e < 15 ? 15 : e;
+  return {__uint_as_float(static_cast<uint32_t>(268 - e) << 23), __uint_as_float(static_cast<uint32_t>(e - 14) << 23)};
+}
+
+// Eight fp32 values as halves of 11 bits each, or as the high ones alone.
+__device__ __forceinline__ void split(const float4v& a, const float4v& b, half8& hi, half8& lo) {
+  half2 h[4], l[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const float x = i < 2 ? a[2 * i] : b[2 * i - 4], y = i < 2 ? a[2 * i + 1] : b[2 * i - 3];
+    h[i] = to_half2(x, y);
+    l[i] = to_half2(x - static_cast<float>(h[i][0]), y - static_cast<float>(h[i][1]));
+  }
+  hi = half8{h[0][0], h[0][1], h[1][0], h[1][1], h[2][0], h[2][1], h[3][0], h[3][1]};
+  lo = half8{l[0][0], l[0][1], l[1][0], l[1][1], l[2][0], l[2][1], l[3][0], l[3][1]};
+}
+__device__ __forceinline__ half8 high(const float4v& a, const float4v& b) {
+  const half2 h0 = to_half2(a[0], a[1]), h1 = to_half2(a[2], a[3]);
+  const half2 h2 = to_half2(b[0], b[1]), h3 = to_half2(b[2], b[3]);
+  return half8{h0[0], h0[1], h1[0], h1[1], h2[0], h2[1], h3[0], h3[1]};
+}
+
+__device__ __forceinline__ int exponent(float v) { return static_cast<int>(__float_as_uint(v) >> 23 & 255); }
+
+__device__ __forceinline__ void wait_for(const int* flag, int at_least) {
+  while (__hip_atomic_load(flag, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP) < at_least)
+    __builtin_amdgcn_s_sleep(1);
+  __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "workgroup");
+}
+__device__ __forceinline__ void publish(int* flag, int value) {
+  __hip_atomic_store(flag, value, __ATOMIC_RELEASE, __HIP_MEMORY_SCOPE_WORKGROUP);
+}
+
+// ------------------------------------------------------------------ prepare
+
+// Sum over the KP / 8 lanes of a token's row (8 or 16 neighbours).
+template <int KP>
+__device__ __forceinline__ float row_sum(float v) {
+  v += dpp<kQuadSwap1>(v);
+  v += dpp<kQuadSwap2>(v);
+  v += dpp<0x141>(v);                    // mirrored within 8 lanes
+  if (KP == 128) v += dpp<0x140>(v);     // mirrored within 16 lanes
+  return v;
+}
+
+// Swaps the 4 x 4 matrix that four registers of the lanes l, l + 16, l + 32
+// and l + 48 hold with its transpose.
+__device__ __forceinline__ void transpose4(uint32_t (&r)[4]) {
+  const auto a = __builtin_amdgcn_permlane32_swap(r[0], r[2], false, false);
+  const auto b = __builtin_amdgcn_permlane32_swap(r[1], r[3], false, false);
+  const auto c = __builtin_amdgcn_permlane16_swap(a[0], b[0], false, false);
+  const auto d = __builtin_amdgcn_permlane16_swap(a[1], b[1], false, false);
+  r[0] = c[0];
+  r[1] = c[1];
+  r[2] = d[0];
+  r[3] = d[1];
+}
+
+// The 32 rows of k or q of a block: a lane loads eight elements (depths 8 c ..)
+// of the tokens 4 lp + l / 16, where c = l % (KP / 8) and lp = kPer i + (l % 16)
+// / (KP / 8) in load i, so that the lanes l, l + 16, l + 32, l + 48 hold four
+// consecutive tokens.
+template <int KP, typename TIn>
+struct Rows {
+  static constexpr int kLanes = KP / 8;
+  static constexpr int kPer = 16 / kLanes;
+  static constexpr int kLoads = 8 / kPer;
+  static constexpr int kWords = sizeof(TIn) == 4 ? 2 : 1;
+  uint4v raw[kLoads][kWords];
+
+  // `first`: the lane's offset in load 0, kDropOffset for lanes beyond K; rows
+  // past `rows` lie past the buffer's end and read as zeros
+  __device__ __forceinline__ void load(const TIn* base, uint32_t first, uint32_t row_bytes, int K, int rows) {
+    const __amdgpu_buffer_rsrc_t r =
+        make_rsrc(base, (rows - 1) * row_bytes + K * static_cast<uint32_t>(sizeof(TIn)));
+#pragma unroll
+    for (int i = 0; i < kLoads; ++i) {
+#pragma unroll
+      for (int w = 0; w < kWords; ++w)
+        raw[i][w] = __builtin_bit_cast(
+            uint4v, __builtin_amdgcn_raw_buffer_load_b128(r, first + 4 * kPer * i * row_bytes + 16 * w, 0, 0));
+    }
+  }
+  static __device__ __forceinline__ uint32_t lane_offset(uint32_t row_bytes, int K) {
+    const int lane = threadIdx.x % 64, c = lane % kLanes;
+    if (8 * c >= K) return kDropOffset;
+    return (4 * (lane % 16 / kLanes) + lane / 16) * row_bytes + 8 * c * static_cast<uint32_t>(sizeof(TIn));
+  }
+  __device__ __forceinline__ void values(int i, float (&v)[8]) const {
+    if constexpr (sizeof(TIn) == 4) {
+#pragma unroll
+      for (int j = 0; j < 8; ++j) v[j] = __uint_as_float(raw[i][j / 4][j % 4]);
+    } else {
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        v[2 * j] = __uint_as_float(raw[i][0][j] << 16);
+        v[2 * j + 1] = __uint_as_float(raw[i][0][j] & 0xffff0000u);
+      }
+    }
+  }
+  // sum of the squares of the lane's eight elements of load i
+  __device__ __forceinline__ float squares(int i, const float (&v)[8]) const {
+    float sq = 0.f;
+    if constexpr (sizeof(TIn) == 4) {
+#pragma unroll
+      for (int j = 0; j < 8; ++j) sq += v[j] * v[j];
+    } else {
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const bf16x2 pair = __builtin_bit_cast(bf16x2, static_cast<uint32_t>(raw[i][0][j]));
+        sq = __builtin_amdgcn_fdot2_f32_bf16(pair, pair, sq, false);
+      }
+    }
+    return sq;
+  }
+};
+
+// The first `count` rows as operands in LDS (and, for keys, transposed ones),
+// and every token's factor: 2^e, divided by the norm where that is asked for.
+template <int KP, bool IN32, bool TRANSPOSE, typename TIn, typename Frags, typename FragsT>
+__device__ __forceinline__ void make_operand(const Rows<KP, TIn>& rows, Frags& frags, FragsT& turned, float* factor,
+                                             int count, int norm, float eps) {
+  using R = Rows<KP, TIn>;
+  const int lane = threadIdx.x % 64, c = lane % R::kLanes, row = lane / 16;
+#pragma unroll
+  for (int i = 0; i < R::kLoads; ++i) {
+    const int lp = R::kPer * i + lane % 16 / R::kLanes, token = 4 * lp + row;
+    float v[8];
+    rows.values(i, v);
+    const float sq = row_sum<KP>(rows.squares(i, v));
+    // 2^e with the scaled norm in [2^6, 2^7)
+    int half_e = static_cast<int>(__float_as_uint(sq) >> 24 & 127);
+    half_e = half_e < 8 ? 8 : half_e;
+    const float up = __uint_as_float(static_cast<uint32_t>(127 + 63 + 6 - half_e) << 23);
+    const float down = __uint_as_float(static_cast<uint32_t>(127 - 63 - 6 + half_e) << 23);
+    if (c == 0) factor[token] = token >= count ? 0.f : norm ? down / sqrtf(sq + eps) : down;
+    uint32_t word[2][4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const float x = v[2 * j] * up, y = v[2 * j + 1] * up;
+      const half2 h = to_half2(x, y);
+      word[0][j] = __builtin_bit_cast(uint32_t, h);
+      if (IN32)
+        word[1][j] = __builtin_bit_cast(
+            uint32_t, to_half2(x - static_cast<float>(h[0]), y - static_cast<float>(h[1])));
+    }
+    const int tile = lp / 4, m = 4 * (lp % 4) + row, q = c % 4;
+#pragma unroll
+    for (int s = 0; s < (IN32 ? 2 : 1); ++s) {
+      // the fragment's 16-byte slots are permuted by q: the 16 lanes of a row
+      // of keys, a quarter of a kilobyte apart, write to different banks
+      frags[s][tile][c / 4][q * 16 + (m ^ 4 * q)] =
+          __builtin_bit_cast(half8, uint4v{word[s][0], word[s][1], word[s][2], word[s][3]});
+      if (TRANSPOSE) {
+        transpose4(word[s]);
+        // now tokens 4 lp .. + 3 of the depths 8 c + 2 row and the next one
+        const uint2v even = {__builtin_amdgcn_perm(word[s][1], word[s][0], 0x05040100),
+                             __builtin_amdgcn_perm(word[s][3], word[s][2], 0x05040100)};
+        const uint2v odd = {__builtin_amdgcn_perm(word[s][1], word[s][0], 0x07060302),
+                            __builtin_amdgcn_perm(word[s][3], word[s][2], 0x07060302)};
+        // state row 32 p + 8 n + 4 h + r is row 4 n + r of row tile 2 p + h
+        const int rt = 2 * (c / 4) + row / 2, rm = 4 * (c % 4) + row % 2 * 2;
+        uint2v* at = reinterpret_cast<uint2v*>(&turned[s][rt][lp % 4 * 16 + rm]) + lp / 4;
+        at[0] = even;
+        at[2] = odd;
+      }
+    }
+  }
+}
+
+template <int KP, bool IN32, bool OUT32, typename TIn>
+__device__ __forceinline__ void prepare_block(const DeltaParams& p, int hk, int h, uint32_t k_off, uint32_t q_off,
+                                              int64_t first, int rows,
+                                              Scratch& s, Buffer<KP, IN32, OUT32>& buf, const int* done, int waves,
+                                              int free_at) {
+  constexpr int kSteps = KP / 32;
+  const int lane = threadIdx.x % 64, m = lane % 16, q = lane / 16;
+  Rows<KP, TIn> kr, qr;
+  kr.load(static_cast<const TIn*>(p.k) + first * p.k_stride + static_cast<int64_t>(hk) * p.K, k_off,
+          static_cast<uint32_t>(p.k_stride * sizeof(TIn)), p.K, rows);
+  const bool outputs = p.o != nullptr;
+  if (outputs)
+    qr.load(static_cast<const TIn*>(p.q) + first * p.q_stride + static_cast<int64_t>(hk) * p.K, q_off,
+            static_cast<uint32_t>(p.q_stride * sizeof(TIn)), p.K, rows);
+  float g = 0.f, beta = 0.f;
+  if (lane < rows) {
+    const int64_t th = (first + lane) * p.Hv + h;
+    g = p.g != nullptr ? p.g[th] : 0.f;
+    g = g < kDeltaErase ? kDeltaErase : g;
+    beta = p.beta != nullptr ? p.beta[th] : 1.f;
+  }
+  for (int w = 0; w < waves; ++w) wait_for(&done[w], free_at);
+
+  double b = static_cast<double>(g);
+#pragma unroll
+  for (int d = 1; d < kBlockTokens; d <<= 1) {
+    const double up = __shfl_up(b, d, kBlockTokens);
+    if (lane % kBlockTokens >= d) b += up;
+  }
+  make_operand<KP, IN32, true, TIn>(kr, buf.k, buf.kt, s.rk, rows, p.norm, p.eps);
+  if (outputs) make_operand<KP, IN32, false, TIn>(qr, buf.q, buf.kt, s.rq, rows, p.norm, p.eps);
+  if (lane < kBlockTokens) {
+    s.b[lane] = b;
+    s.beta[lane] = beta;
+  }
+  wave_fence();
+
+  // k_i.k_j and q_i.k_j with i in the lanes and j = 4 q + r in the registers
+  float4v kk[3] = {}, qk[3] = {};  // tiles (0, 0), (1, 0), (1, 1)
+#pragma unroll
+  for (int st = 0; st < kSteps; ++st) {
+    const int at = q * 16 + (m ^ 4 * q);
+    half8 kf[2], qf[2];
+#pragma unroll
+    for (int t = 0; t < 2; ++t) {
+      kf[t] = buf.k[0][t][st][at];
+      if (outputs) qf[t] = buf.q[0][t][st][at];
+    }
+#pragma unroll
+    for (int i = 0; i < 3; ++i) kk[i] = mfma(kf[i / 2], kf[i > 0], kk[i]);
+    if (outputs) {
+#pragma unroll
+      for (int i = 0; i < 3; ++i) qk[i] = mfma(kf[i / 2], qf[i > 0], qk[i]);
+    }
+    if (IN32) {
+      half8 kl[2], ql[2];
+#pragma unroll
+      for (int t = 0; t < 2; ++t) {
+        kl[t] = buf.k[Buffer<KP, IN32, OUT32>::kHalves - 1][t][st][at];
+        if (outputs) ql[t] = buf.q[Buffer<KP, IN32, OUT32>::kHalves - 1][t][st][at];
+      }
+#pragma unroll
+      for (int i = 0; i < 3; ++i) {
+        kk[i] = mfma(kl[i / 2], kf[i > 0], kk[i]);
+        kk[i] = mfma(kf[i / 2], kl[i > 0], kk[i]);
+        if (outputs) {
+          qk[i] = mfma(kl[i / 2], qf[i > 0], qk[i]);
+          qk[i] = mfma(kf[i / 2], ql[i > 0], qk[i]);
+        }
+      }
+    }
+  }
+  float4v pm[3];
+#pragma unroll
+  for (int i = 0; i < 3; ++i) {
+    const int ti = i > 0, tj = i / 2, row = 16 * ti + m;
+    const double bi = s.b[row];
+    const float ri = s.rk[row] * s.beta[row];
+    float4v a;
+#pragma unroll
+    for (int r = 0; r < 4; ++r) {
+      const int col = 16 * tj + 4 * q + r;
+      const float decay = __builtin_amdgcn_exp2f(static_cast<float>(bi - s.b[col]) * kLog2e);
+      a[r] = row > col ? ri * s.rk[col] * (decay * kk[i][r]) : 0.f;
+      pm[i][r] = row >= col ? decay * qk[i][r] : 0.f;
+    }
+    *reinterpret_cast<float4v*>(&s.a[row * kAStride + 16 * tj + 4 * q]) = a;
+  }
+  if (outputs) {
+    const float4v none = {};
+#pragma unroll
+    for (int t = 0; t < 2; ++t) {
+      half8 hi, lo;
+      split(pm[t], t ? pm[2] : none, hi, lo);
+      buf.p[0][t][lane] = hi;
+      if (OUT32) buf.p[OUT32][t][lane] = lo;
+    }
+  }
+  wave_fence();
+
+  // (I + A)^-1 of the two diagonal 16 x 16 blocks: lane l has column l % 16 of
+  // block l / 16 (the upper lanes repeat the lower ones)
+  const int blk = q & 1;
+  float col[16];
+  const float* diag = &s.a[16 * blk * kAStride + 16 * blk];
+#pragma unroll
+  for (int i = 0; i < 16; ++i) {
+    float sum = i == m ? 1.f : 0.f;
+#pragma unroll
+    for (int j4 = 0; j4 < (i + 3) / 4; ++j4) {
+      const float4v a = *reinterpret_cast<const float4v*>(&diag[i * kAStride + 4 * j4]);
+#pragma unroll
+      for (int j = 0; j < 4; ++j)
+        if (4 * j4 + j < i) sum -= a[j] * col[4 * j4 + j];
+    }
+    col[i] = sum;
+  }
+  wave_fence();
+  if (lane < 32) {
+#pragma unroll
+    for (int i = 0; i < 16; ++i) s.a[(16 * blk + i) * kAStride + 16 * blk + m] = col[i];
+  }
+  wave_fence();
+  // the lower left one: -T22 A21 T11, in fp32
+  float4v y = {}, z = {};
+#pragma unroll
+  for (int st = 0; st < 4; ++st)
+    y = mfma(s.a[(16 + m) * kAStride + 4 * st + q], s.a[(4 * st + q) * kAStride + m], y);
+  const float4v t22 = *reinterpret_cast<const float4v*>(&s.a[(16 + m) * kAStride + 16 + 4 * q]);
+#pragma unroll
+  for (int st = 0; st < 4; ++st) z = mfma(t22[st], y[st], z);
+  wave_fence();
+#pragma unroll
+  for (int r = 0; r < 4; ++r) s.a[(16 + 4 * q + r) * kAStride + m] = -z[r];
+  wave_fence();
+  {
+    const float4v beta0 = *reinterpret_cast<const float4v*>(&s.beta[4 * q]);
+    const float4v beta1 = *reinterpret_cast<const float4v*>(&s.beta[16 + 4 * q]);
+    const float4v none = {};
+    const float4v t11 = *reinterpret_cast<const float4v*>(&s.a[m * kAStride + 4 * q]) * beta0;
+    const float4v t21 = *reinterpret_cast<const float4v*>(&s.a[(16 + m) * kAStride + 4 * q]) * beta0;
+    const float4v tt2 = t22 * beta1;
+    float most = 0.f;
+#pragma unroll
+    for (int r = 0; r < 4; ++r) most = max_abs(max_abs(max_abs(most, t11[r]), t21[r]), tt2[r]);
+    const Scale sc = scale_of(wave_max(most));
+    half8 hi, lo;
+    split(t11 * sc.up, none, hi, lo);
+    buf.t[0][0][lane] = hi;
+    buf.t[1][0][lane] = lo;
+    split(t21 * sc.up, tt2 * sc.up, hi, lo);
+    buf.t[0][1][lane] = hi;
+    buf.t[1][1][lane] = lo;
+    const int token = lane % kBlockTokens;
+    const double end = s.b[kBlockTokens - 1];
+    const float rk = s.rk[token], fo = outputs ? p.scale * s.rq[token] : 0.f;
+    const float eb = __builtin_amdgcn_exp2f(static_cast<float>(b) * kLog2e);
+    const float fu = rk * __builtin_amdgcn_exp2f(static_cast<float>(end - b) * kLog2e);
+    const float largest = wave_max(fmaxf(rk, fu));
+    if (lane < kBlockTokens) {
+      buf.f.x[lane] = rk * eb;
+      buf.f.r[lane] = rk;
+      buf.f.u[lane] = fu;
+      buf.f.q[lane] = fo * eb;
+      buf.f.o[lane] = fo;
+      if (lane == kBlockTokens - 1) buf.f.decay = eb;
+      if (lane == 0) {
+        buf.f.t = sc.down;
+        buf.f.most = largest;
+      }
+    }
+  }
+  wave_fence();
+}
+
+// -------------------------------------------------------------------- chain
+
+// NV neighbouring elements at a byte offset of a buffer, and NV results to one.
+template <typename T, int NV>
+__device__ __forceinline__ void load_cols(__amdgpu_buffer_rsrc_t r, uint32_t off, uint32_t (&raw)[2]) {
+  constexpr int kBytes = static_cast<int>(sizeof(T)) * NV;
+  if constexpr (kBytes == 2) {
+    raw[0] = static_cast<uint16_t>(__builtin_amdgcn_raw_buffer_load_b16(r, off, 0, 0));
+  } else if constexpr (kBytes == 4) {
+    raw[0] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_raw_buffer_load_b32(r, off, 0, 0));
+  } else {
+    const uint2v v = __builtin_bit_cast(uint2v, __builtin_amdgcn_raw_buffer_load_b64(r, off, 0, 0));
+    raw[0] = v[0];
+    raw[1] = v[1];
+  }
+}
+template <typename T>
+__device__ __forceinline__ float col_value(const uint32_t (&raw)[2], int n) {
+  if constexpr (sizeof(T) == 4) return __uint_as_float(raw[n]);
+  return __uint_as_float(n ? raw[0] & 0xffff0000u : raw[0] << 16);
+}
+template <typename T, int NV>
+__device__ __forceinline__ void store_cols(__amdgpu_buffer_rsrc_t r, uint32_t off, const float (&v)[NV]) {
+  if constexpr (sizeof(T) == 4) {
+    if constexpr (NV == 1)
+      __builtin_amdgcn_raw_buffer_store_b32(__float_as_uint(v[0]), r, off, 0, 0);
+    else
+      __builtin_amdgcn_raw_buffer_store_b64(uint2v{__float_as_uint(v[0]), __float_as_uint(v[1])}, r, off, 0, 0);
+  } else {
+    if constexpr (NV == 1)
+      __builtin_amdgcn_raw_buffer_store_b16(narrow<bf16_t>(v[0]).bits, r, off, 0, 0);
+    else
+      __builtin_amdgcn_raw_buffer_store_b32(
+          narrow<bf16_t>(v[0]).bits | static_cast<uint32_t>(narrow<bf16_t>(v[1]).bits) << 16, r, off, 0, 0);
+  }
+}
+
+// The states of a wave's columns: rows of tile t, register r are the state row
+// 32 (t / 2) + 8 q + 4 (t % 2) + r, columns col .. col + NV - 1.
+template <int KP, int NV, typename TSt>
+__device__ __forceinline__ void load_state(const TSt* base, int64_t V, int K, int col, float4v (&S)[NV][KP / 16]) {
+  const int q = threadIdx.x % 64 / 16;
+#pragma unroll
+  for (int t = 0; t < KP / 16; ++t) {
+#pragma unroll
+    for (int r = 0; r < 4; ++r) {
+      const int row = 32 * (t / 2) + 8 * q + 4 * (t % 2) + r;
+      if (row < K && col < V) {
+        const Pack<TSt, NV> v = load_pack<NV>(base + row * V + col);
+#pragma unroll
+        for (int n = 0; n < NV; ++n) S[n][t][r] = widen(v.v[n]);
+      }
+    }
+  }
+}
+template <int KP, int NV, typename TSt>
+__device__ __forceinline__ void store_state(TSt* base, int64_t V, int K, int col, const float4v (&S)[NV][KP / 16]) {
+  const int q = threadIdx.x % 64 / 16;
+#pragma unroll
+  for (int t = 0; t < KP / 16; ++t) {
+#pragma unroll
+    for (int r = 0; r < 4; ++r) {
+      const int row = 32 * (t / 2) + 8 * q + 4 * (t % 2) + r;
+      if (row < K && col < V) {
+        float v[NV];
+#pragma unroll
+        for (int n = 0; n < NV; ++n) v[n] = S[n][t][r];
+        store_pack<NV>(base + row * V + col, v);
+      }
+    }
+  }
+}
+
+template <int KP, bool IN32, bool OUT32, int NV>
+__global__ void __launch_bounds__(64 * (kChainMax + Shared<KP, IN32, OUT32>::kPrepare))
+    delta_kernel(DeltaParams p, int chain_waves, int state16) {
+  using TIn = std::conditional_t<IN32, float, bf16_t>;
+  using TOut = std::conditional_t<OUT32, float, bf16_t>;
+  using Sh = Shared<KP, IN32, OUT32>;
+  using Buf = Buffer<KP, IN32, OUT32>;
+  constexpr int kSteps = KP / 32, kTiles = KP / 16, kLow = Buf::kHalves - 1;
+  static_assert(sizeof(Sh) <= 160 * 1024, "LDS of a CU");
+  __shared__ __align__(16) unsigned char lds[sizeof(Sh)];
+  Sh& sh = *reinterpret_cast<Sh*>(lds);
+
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
+  const int lane = threadIdx.x % 64, m = lane % 16, q = lane / 16;
+  const int width = 16 * NV * chain_waves;
+  const int vblocks = (p.V + width - 1) / width;
+  // the heads that share keys follow one another, on one XCD
+  const int bid = xcd_remap(blockIdx.x, gridDim.x);
+  const int vb = bid % vblocks;
+  const int h = bid / vblocks % p.Hv;
+  const int64_t b = bid / vblocks / p.Hv;
+  const Span span = sequence(p.starts, b, p.L, p.T);
+  const int blocks = static_cast<int>((span.end - span.begin + kBlockTokens - 1) / kBlockTokens);
+
+  if (threadIdx.x < Sh::kBuffers) sh.ready[threadIdx.x] = 0;
+  if (threadIdx.x < kChainMax) sh.done[threadIdx.x] = 0;
+  __syncthreads();
+
+  if (wave >= chain_waves) {
+    const int hk = h / (p.Hv / p.Hk);
+    const int self = wave - chain_waves;
+    const uint32_t k_off = Rows<KP, TIn>::lane_offset(static_cast<uint32_t>(p.k_stride * sizeof(TIn)), p.K);
+    const uint32_t q_off = Rows<KP, TIn>::lane_offset(static_cast<uint32_t>(p.q_stride * sizeof(TIn)), p.K);
+    for (int c = self; c < blocks; c += Sh::kPrepare) {
+      const int64_t first = span.begin + static_cast<int64_t>(c) * kBlockTokens;
+      const int64_t left = span.end - first;
+      const int rows = left < kBlockTokens ? static_cast<int>(left) : kBlockTokens;
+      prepare_block<KP, IN32, OUT32, TIn>(p, hk, h, k_off, q_off, first, rows, sh.scratch[self], sh.buf[c % Sh::kBuffers], sh.done,
+                                          chain_waves, c - Sh::kBuffers + 1);
+      publish(&sh.ready[c % Sh::kBuffers], c + 1);
+    }
+    return;
+  }
+
+  const int col = vb * width + wave * 16 * NV + m * NV;
+  if (vb * width + wave * 16 * NV >= p.V) {  // no columns: the prepare waves need not wait
+    publish(&sh.done[wave], 0x7fffffff);
+    return;
+  }
+  const int64_t state_at = static_cast<int64_t>(h) * p.K * p.V;
+  float4v S[NV][kTiles] = {};
+  {
+    int64_t row = b;
+    bool known = true;
+    if (p.idx != nullptr) {
+      row = p.idx[b];
+      known = row >= 0 && row < p.state_rows;
+    }
+    if (!known) {
+      const float nan = __builtin_nanf("");
+#pragma unroll
+      for (int n = 0; n < NV; ++n)
+#pragma unroll
+        for (int t = 0; t < kTiles; ++t) S[n][t] = float4v{nan, nan, nan, nan};
+    } else if (p.h0 != nullptr) {
+      if (state16)
+        load_state<KP, NV>(static_cast<const f16_t*>(p.h0) + row * p.h0_stride + state_at, p.V, p.K, col, S);
+      else
+        load_state<KP, NV>(static_cast<const float*>(p.h0) + row * p.h0_stride + state_at, p.V, p.K, col, S);
+    }
+  }
+
+  const bool outputs = p.o != nullptr;
+  const uint32_t v_step = static_cast<uint32_t>(p.v_stride * sizeof(TIn));
+  const uint32_t o_step = static_cast<uint32_t>(static_cast<int64_t>(p.Hv) * p.V * sizeof(TOut));
+  const uint32_t v_off = col < p.V ? static_cast<uint32_t>(col * sizeof(TIn)) + 4 * q * v_step : kDropOffset;
+  const uint32_t o_off = col < p.V ? static_cast<uint32_t>(col * sizeof(TOut)) + 4 * q * o_step : kDropOffset;
+  uint32_t raw[2][4][2];  // the block's values: tokens 16 t + 4 q + r
+  const auto fetch = [&](int c) {
+    const int64_t first = span.begin + static_cast<int64_t>(c) * kBlockTokens, left = span.end - first;
+    const uint32_t rows = left < kBlockTokens ? static_cast<uint32_t>(left) : kBlockTokens;
+    const __amdgpu_buffer_rsrc_t r =
+        make_rsrc(static_cast<const TIn*>(p.v) + first * p.v_stride + static_cast<int64_t>(h) * p.V,
+                  (rows - 1) * v_step + p.V * static_cast<uint32_t>(sizeof(TIn)));
+#pragma unroll
+    for (int t = 0; t < 2; ++t)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) load_cols<TIn, NV>(r, v_off + (16 * t + i) * v_step, raw[t][i]);
+  };
+  if (blocks > 0) fetch(0);
+
+  // A column of S is held as S~ = S / sigma, sigma a power of two such that
+  // |S~| < 2^16: its halves are fp16 numbers as they are.  `bound` >= |S~|.
+  // A block multiplies S~ by decay sigma / sigma' and adds K^T (U / sigma'),
+  // where 32 keys' elements of at most 2^7 meet |U / sigma'| < 2^2: sigma' is
+  // chosen so that both terms stay below 2^14.  The halves' floor of 2^-24
+  // leaves them 22 bits of the column's largest while it is above 2^-2, and the
+  // bound, which is some 2^6 above it and can grow by 2^14 a block, is taken
+  // anew from S~ every eighth block.
+  float sigma[NV], bound[NV];
+  const auto largest = [&](int n) {
+    float most = 0.f;
+#pragma unroll
+    for (int t = 0; t < kTiles; ++t)
+#pragma unroll
+      for (int r = 0; r < 4; ++r) most = max_abs(most, S[n][t][r]);
+    return max_of_rows(most);
+  };
+#pragma unroll
+  for (int n = 0; n < NV; ++n) {
+    const float most = largest(n);
+    const Scale sc = scale_of(most);
+    sigma[n] = sc.down;
+    bound[n] = most * sc.up;
+#pragma unroll
+    for (int t = 0; t < kTiles; ++t) S[n][t] *= sc.up;
+  }
+
+  for (int c = 0; c < blocks; ++c) {
+    const int64_t first = span.begin + static_cast<int64_t>(c) * kBlockTokens, left = span.end - first;
+    // the state as an operand
+    half8 s_hi[NV][kSteps], s_lo[NV][kSteps];
+#pragma unroll
+    for (int n = 0; n < NV; ++n)
+#pragma unroll
+      for (int st = 0; st < kSteps; ++st) split(S[n][2 * st], S[n][2 * st + 1], s_hi[n][st], s_lo[n][st]);
+    const Buf& buf = sh.buf[c % Sh::kBuffers];
+    wait_for(&sh.ready[c % Sh::kBuffers], c + 1);
+
+    // K S and Q S
+    float4v ks[2][NV] = {}, qs[2][NV] = {};
+#pragma unroll
+    for (int st = 0; st < kSteps; ++st) {
+      const int at = q * 16 + (m ^ 4 * q);
+#pragma unroll
+      for (int t = 0; t < 2; ++t) {
+        const half8 kf = buf.k[0][t][st][at];
+#pragma unroll
+        for (int n = 0; n < NV; ++n) {
+          ks[t][n] = mfma(kf, s_hi[n][st], ks[t][n]);
+          ks[t][n] = mfma(kf, s_lo[n][st], ks[t][n]);
+        }
+        if (IN32) {
+          const half8 kl = buf.k[kLow][t][st][at];
+#pragma unroll
+          for (int n = 0; n < NV; ++n) ks[t][n] = mfma(kl, s_hi[n][st], ks[t][n]);
+        }
+        if (outputs) {
+          const half8 qf = buf.q[0][t][st][at];
+#pragma unroll
+          for (int n = 0; n < NV; ++n) {
+            qs[t][n] = mfma(qf, s_hi[n][st], qs[t][n]);
+            if (OUT32) qs[t][n] = mfma(qf, s_lo[n][st], qs[t][n]);
+          }
+          if (IN32 && OUT32) {
+            const half8 ql = buf.q[kLow][t][st][at];
+#pragma unroll
+            for (int n = 0; n < NV; ++n) qs[t][n] = mfma(ql, s_hi[n][st], qs[t][n]);
+          }
+        }
+      }
+    }
+    // X, then U = T X without the powers of two of their operands
+    float4v u[2][NV] = {};
+    float u_unit[NV];
+    {
+      float4v x[2][NV];
+#pragma unroll
+      for (int t = 0; t < 2; ++t) {
+        const float4v fx = *reinterpret_cast<const float4v*>(&buf.f.x[16 * t + 4 * q]);
+#pragma unroll
+        for (int n = 0; n < NV; ++n)
+#pragma unroll
+          for (int r = 0; r < 4; ++r) x[t][n][r] = col_value<TIn>(raw[t][r], n) - fx[r] * sigma[n] * ks[t][n][r];
+      }
+      if (c + 1 < blocks) fetch(c + 1);
+      half8 x_hi[NV], x_lo[NV];
+#pragma unroll
+      for (int n = 0; n < NV; ++n) {
+        float most = 0.f;
+#pragma unroll
+        for (int t = 0; t < 2; ++t)
+#pragma unroll
+          for (int r = 0; r < 4; ++r) most = max_abs(most, x[t][n][r]);
+        const Scale sc = scale_of(max_of_rows(most));
+        u_unit[n] = sc.down * buf.f.t;
+        split(x[0][n] * sc.up, x[1][n] * sc.up, x_hi[n], x_lo[n]);
+      }
+#pragma unroll
+      for (int t = 0; t < 2; ++t) {
+        const half8 t_hi = buf.t[0][t][lane], t_lo = buf.t[1][t][lane];
+#pragma unroll
+        for (int n = 0; n < NV; ++n) {
+          u[t][n] = mfma(t_hi, x_hi[n], u[t][n]);
+          u[t][n] = mfma(t_hi, x_lo[n], u[t][n]);
+          u[t][n] = mfma(t_lo, x_hi[n], u[t][n]);
+        }
+      }
+    }
+    // U / sigma' as two operands: |k| U for Q K^T, e^{b_end - b} |k| U for K^T
+    half8 u_hi[NV], u_lo[NV], w_hi[NV], w_lo[NV];
+    float next[NV], keep[NV];  // sigma', and the factor of S~
+    {
+      float4v fr[2], fu[2];
+#pragma unroll
+      for (int t = 0; t < 2; ++t) {
+        fr[t] = *reinterpret_cast<const float4v*>(&buf.f.r[16 * t + 4 * q]);
+        fu[t] = *reinterpret_cast<const float4v*>(&buf.f.u[16 * t + 4 * q]);
+      }
+      const float f_most = buf.f.most, decay = buf.f.decay;
+#pragma unroll
+      for (int n = 0; n < NV; ++n) {
+        float most = 0.f;
+#pragma unroll
+        for (int t = 0; t < 2; ++t)
+#pragma unroll
+          for (int r = 0; r < 4; ++r) most = max_abs(most, u[t][n][r]);
+        most = max_of_rows(most) * f_most * u_unit[n];
+        // the last term bounds sigma / sigma' by 2^64 where S and U vanish
+        int e = exponent(most) - 1;
+        e = max(e, exponent(bound[n] * sigma[n] * decay) - 13);
+        e = max(e, exponent(sigma[n]) - 64);
+        e = min(max(e, 2), 252);
+        next[n] = __uint_as_float(static_cast<uint32_t>(e) << 23);
+        const float up = __uint_as_float(static_cast<uint32_t>(254 - e) << 23);
+        keep[n] = sigma[n] * up * decay;
+        bound[n] = bound[n] * keep[n] + 4096.f * (most * up);
+        const float unit = u_unit[n] * up;
+        u[0][n] *= unit;
+        u[1][n] *= unit;
+        split(u[0][n] * fu[0], u[1][n] * fu[1], u_hi[n], u_lo[n]);
+        if (OUT32)
+          split(u[0][n] * fr[0], u[1][n] * fr[1], w_hi[n], w_lo[n]);
+        else
+          w_hi[n] = high(u[0][n] * fr[0], u[1][n] * fr[1]);
+      }
+    }
+    if (outputs) {
+      const uint32_t rows = left < kBlockTokens ? static_cast<uint32_t>(left) : kBlockTokens;
+      const __amdgpu_buffer_rsrc_t ro =
+          make_rsrc(static_cast<TOut*>(p.o) + (first * p.Hv + h) * p.V,
+                    (rows - 1) * o_step + p.V * static_cast<uint32_t>(sizeof(TOut)));
+#pragma unroll
+      for (int t = 0; t < 2; ++t) {
+        const half8 pf = buf.p[0][t][lane];
+        float4v pu[NV] = {};
+#pragma unroll
+        for (int n = 0; n < NV; ++n) {
+          pu[n] = mfma(pf, w_hi[n], pu[n]);
+          if (OUT32) {
+            pu[n] = mfma(pf, w_lo[n], pu[n]);
+            pu[n] = mfma(buf.p[OUT32][t][lane], w_hi[n], pu[n]);
+          }
+        }
+        const float4v fq = *reinterpret_cast<const float4v*>(&buf.f.q[16 * t + 4 * q]);
+        const float4v fo = *reinterpret_cast<const float4v*>(&buf.f.o[16 * t + 4 * q]);
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+          float v[NV];
+#pragma unroll
+          for (int n = 0; n < NV; ++n)
+            v[n] = fq[r] * (sigma[n] * qs[t][n][r]) + fo[r] * (next[n] * pu[n][r]);
+          store_cols<TOut, NV>(ro, o_off + (16 * t + r) * o_step, v);
+        }
+      }
+    }
+#pragma unroll
+    for (int t = 0; t < kTiles; ++t) {
+      const half8 kf = buf.kt[0][t][lane];
+#pragma unroll
+      for (int n = 0; n < NV; ++n) {
+        S[n][t] *= keep[n];
+        S[n][t] = mfma(kf, u_hi[n], S[n][t]);
+        S[n][t] = mfma(kf, u_lo[n], S[n][t]);
+        if (IN32) S[n][t] = mfma(buf.kt[kLow][t][lane], u_hi[n], S[n][t]);
+      }
+    }
+#pragma unroll
+    for (int n = 0; n < NV; ++n) sigma[n] = next[n];
+    if (c % 8 == 7) {
+#pragma unroll
+      for (int n = 0; n < NV; ++n) bound[n] = largest(n);
+    }
+    publish(&sh.done[wave], c + 1);
+  }
+
+  if (p.hT != nullptr) {
+#pragma unroll
+    for (int n = 0; n < NV; ++n)
+#pragma unroll
+      for (int t = 0; t < kTiles; ++t) S[n][t] *= sigma[n];
+    if (state16)
+      store_state<KP, NV>(static_cast<f16_t*>(p.hT) + b * p.hT_stride + state_at, p.V, p.K, col, S);
+    else
+      store_state<KP, NV>(static_cast<float*>(p.hT) + b * p.hT_stride + state_at, p.V, p.K, col, S);
+  }
+}
+
+template <int KP, bool IN32, bool OUT32, int NV>
+hipError_t launch_typed(const DeltaParams& p, int chain_waves, int state16, hipStream_t s) {
+  using Sh = Shared<KP, IN32, OUT32>;
+  const int width = 16 * NV * chain_waves;
+  const int64_t grid = p.B * p.Hv * ((p.V + width - 1) / width);
+  delta_kernel<KP, IN32, OUT32, NV>
+      <<<dim3(static_cast<uint32_t>(grid)), 64 * (chain_waves + Sh::kPrepare), 0, s>>>(p, chain_waves, state16);
+  return hipGetLastError();
+}
+
+}  // namespace
+
+hipError_t launch_delta(const DeltaParams& p, int in_dtype, int out_dtype, int state_dtype, int cus, hipStream_t s) {
+  // Columns of a workgroup.  All of a head's (up to 128) where the heads alone
+  // fill the CUs; else fewer, so that more workgroups run the chain of a head.
+  int nv = 2, waves = (p.V + 31) / 32;
+  if (waves > kChainMax) waves = kChainMax;
+  if (p.B * p.Hv * ((p.V + 32 * waves - 1) / (32 * waves)) < cus) {
+    waves = 1;
+    if (p.B * p.Hv * ((p.V + 31) / 32) < cus) nv = 1;
+  }
+  const int state16 = state_dtype == PRECOG_F16;
+  const auto go = [&](auto kp, auto in32, auto out32) {
+    constexpr int KP = decltype(kp)::value;
+    constexpr bool IN32 = decltype(in32)::value, OUT32 = decltype(out32)::value;
+    return nv == 2 ? launch_typed<KP, IN32, OUT32, 2>(p, waves, state16, s)
+                   : launch_typed<KP, IN32, OUT32, 1>(p, waves, state16, s);
+  };
+  const auto sized = [&](auto in32, auto out32) {
+    return p.K <= 64 ? go(std::integral_constant<int, 64>{}, in32, out32)
+                     : go(std::integral_constant<int, 128>{}, in32, out32);
+  };
+  using Yes = std::true_type;
+  using No = std::false_type;
+  if (in_dtype == PRECOG_F32) return out_dtype == PRECOG_F32 ? sized(Yes{}, Yes{}) : sized(Yes{}, No{});
+  return out_dtype == PRECOG_F32 ? sized(No{}, Yes{}) : sized(No{}, No{});
+}
+
+}  // namespace precog

@@ -191,9 +191,4 @@ hipError_t launch_delta_step(const DeltaParams& p, int in_dtype, int out_dtype, 
   return by_types<true>(p, in_dtype, out_dtype, state_dtype, cus, s);
 }
 
-hipError_t launch_delta(const DeltaParams& p, int in_dtype, int out_dtype, int state_dtype, int cus,
-                        hipStream_t s) {
-  return by_types<false>(p, in_dtype, out_dtype, state_dtype, cus, s);
-}
-
 }  // namespace precog

@@ -27,6 +27,13 @@ def delta_bar(tokens):
     return 5 * 2.0 ** -20.5 * math.sqrt(1 + tokens / 32)
 
 
+# What a bf16 o may have more than delta_bar, against its rms: its two terms Q S
+# and Q K^T U take operands of 11 bits (errors of at most 2^-12 each, 2^-12 / sqrt(3)
+# rms: S in the one, two in the other), together 2^-12 of the terms' rms, which are
+# up to 1.5 times o's where they partly cancel; five times that is 2^-9.1.
+O16 = 2.0 ** -9
+
+
 def check(got, ref, bar, what=""):
     """|got - ref| <= half a step of got's type + bar * max(|ref|, rms(ref))."""
     t = got.dtype
