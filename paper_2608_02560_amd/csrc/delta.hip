@@ -39,13 +39,13 @@
 #include "layer_ops.h"
 #include "wave_ops.h"
 
+#include <type_traits>
+
 namespace precog {
 namespace {
 
 constexpr int kBlockTokens = 32;
 constexpr int kChainMax = 4;     // chain waves of a workgroup
-constexpr int kAStride = 36;     // floats between rows of A in LDS: 16-byte rows on shifting banks
-constexpr float kLog2e = 1.44269504088896341f;
 
 typedef _Float16 half8 __attribute__((ext_vector_type(8)));
 typedef _Float16 half4 __attribute__((ext_vector_type(4)));
@@ -69,33 +69,42 @@ struct Factors {
   float pad;
 };
 
+// What a call computes beside the states.
+constexpr int kNoOutput = 0, kOut16 = 1, kOut32 = 2;
+
 // A block's operands in LDS, in 1 KB fragments of one matrix instruction.
-template <int KP, bool IN32, bool OUT32>
+template <int KP, bool IN32, int OUT>
 struct Buffer {
   static constexpr int kHalves = IN32 ? 2 : 1;
   static constexpr int kSteps = KP / 32;
   half8 k[kHalves][2][kSteps][64];    // token tile, depth step
-  half8 q[kHalves][2][kSteps][64];
+  half8 q[OUT ? kHalves : 0][2][kSteps][64];
   half8 kt[kHalves][KP / 16][64];     // state row tile; depth: the block's tokens
   half8 t[2][2][64];                  // half, token tile
-  half8 p[OUT32 ? 2 : 1][2][64];
+  half8 p[OUT][2][64];                // half, token tile
   Factors f;
 };
 
-// A prepare wave's own LDS.
+// A prepare wave's own LDS.  b log2(e) is the sum of two floats, so that
+// differences of it are good to 2^-24 of themselves.
 struct Scratch {
-  float a[kBlockTokens * kAStride];
-  double b[kBlockTokens];
+  float b[kBlockTokens], b_low[kBlockTokens];
   float rk[kBlockTokens];
   float rq[kBlockTokens];
   float beta[kBlockTokens];
 };
 
-template <int KP, bool IN32, bool OUT32>
+// A and its inverse, 32 x 32 floats, take the place of T's operands until these
+// are made.  Groups of four columns are permuted within a row, so that 16 lanes
+// that read a column of groups meet different banks.
+__device__ __forceinline__ int a_at(int row, int col) { return 32 * row + 4 * (col / 4 ^ row % 8) + col % 4; }
+
+template <int KP, bool IN32, int OUT>
 struct Shared {
-  static constexpr int kBuffers = IN32 ? 2 : 4;   // as many as fit into 160 KB
+  // as many as fit into the 160 KB of a CU, up to five
+  static constexpr int kBuffers = IN32 ? 2 : KP == 128 && OUT == kOut32 ? 4 : 5;
   static constexpr int kPrepare = kBuffers - 1;   // prepare waves: each works on a buffer of its own
-  Buffer<KP, IN32, OUT32> buf[kBuffers];
+  Buffer<KP, IN32, OUT> buf[kBuffers];
   Scratch scratch[kPrepare];
   int ready[kBuffers];       // block held by the buffer, counted from 1
   int done[kChainMax];       // blocks that the chain wave has read
@@ -116,6 +125,14 @@ __device__ __forceinline__ half2 to_half2(float a, float b) {
 __device__ __forceinline__ void wave_fence() {
   __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
   __builtin_amdgcn_wave_barrier();
+}
+
+// The lane's number as a value of its own: what is computed from it is not kept
+// in registers from one part of a long function to the next.
+__device__ __forceinline__ int fresh_lane() {
+  int lane = threadIdx.x % 64;
+  asm volatile("" : "+v"(lane));
+  return lane;
 }
 
 __device__ __forceinline__ float max_abs(float m, float v) { return fmaxf(m, fabsf(v)); }
@@ -212,6 +229,8 @@ struct Rows {
   __device__ __forceinline__ void load(const TIn* base, uint32_t first, uint32_t row_bytes, int K, int rows) {
     const __amdgpu_buffer_rsrc_t r =
         make_rsrc(base, (rows - 1) * row_bytes + K * static_cast<uint32_t>(sizeof(TIn)));
+    // the loads' offsets are cheaper made than kept
+    asm volatile("" : "+v"(first));
 #pragma unroll
     for (int i = 0; i < kLoads; ++i) {
 #pragma unroll
@@ -254,25 +273,34 @@ struct Rows {
   }
 };
 
-// The first `count` rows as operands in LDS (and, for keys, transposed ones),
-// and every token's factor: 2^e, divided by the norm where that is asked for.
+// A row's power of two: its norm times `up` is in [2^6, 2^7).
+__device__ __forceinline__ Scale row_scale(float sq) {
+  int half_e = static_cast<int>(__float_as_uint(sq) >> 24 & 127);
+  half_e = half_e < 8 ? 8 : half_e;
+  return {__uint_as_float(static_cast<uint32_t>(127 + 63 + 6 - half_e) << 23),
+          __uint_as_float(static_cast<uint32_t>(127 - 63 - 6 + half_e) << 23)};
+}
+// What a row's operand lacks: that power of two, over the norm where the row is
+// to be normalised.
+__device__ __forceinline__ float row_factor(float sq, int norm, float eps) {
+  const float down = row_scale(sq).down;
+  return norm ? down * __builtin_amdgcn_rsqf(sq + eps) : down;
+}
+
+// Rows as operands in LDS (and, for keys, transposed ones), and every token's
+// sum of squares.
 template <int KP, bool IN32, bool TRANSPOSE, typename TIn, typename Frags, typename FragsT>
-__device__ __forceinline__ void make_operand(const Rows<KP, TIn>& rows, Frags& frags, FragsT& turned, float* factor,
-                                             int count, int norm, float eps) {
+__device__ __forceinline__ void make_operand(const Rows<KP, TIn>& rows, Frags& frags, FragsT& turned, float* squares) {
   using R = Rows<KP, TIn>;
-  const int lane = threadIdx.x % 64, c = lane % R::kLanes, row = lane / 16;
+  const int lane = fresh_lane(), c = lane % R::kLanes, row = lane / 16;
 #pragma unroll
   for (int i = 0; i < R::kLoads; ++i) {
-    const int lp = R::kPer * i + lane % 16 / R::kLanes, token = 4 * lp + row;
+    const int lp = R::kPer * i + lane % 16 / R::kLanes;
     float v[8];
     rows.values(i, v);
     const float sq = row_sum<KP>(rows.squares(i, v));
-    // 2^e with the scaled norm in [2^6, 2^7)
-    int half_e = static_cast<int>(__float_as_uint(sq) >> 24 & 127);
-    half_e = half_e < 8 ? 8 : half_e;
-    const float up = __uint_as_float(static_cast<uint32_t>(127 + 63 + 6 - half_e) << 23);
-    const float down = __uint_as_float(static_cast<uint32_t>(127 - 63 - 6 + half_e) << 23);
-    if (c == 0) factor[token] = token >= count ? 0.f : norm ? down / sqrtf(sq + eps) : down;
+    const float up = row_scale(sq).up;
+    if (c == 0) squares[4 * lp + row] = sq;
     uint32_t word[2][4];
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
@@ -307,43 +335,70 @@ __device__ __forceinline__ void make_operand(const Rows<KP, TIn>& rows, Frags& f
   }
 }
 
-template <int KP, bool IN32, bool OUT32, typename TIn>
-__device__ __forceinline__ void prepare_block(const DeltaParams& p, int hk, int h, uint32_t k_off, uint32_t q_off,
-                                              int64_t first, int rows,
-                                              Scratch& s, Buffer<KP, IN32, OUT32>& buf, const int* done, int waves,
-                                              int free_at) {
-  constexpr int kSteps = KP / 32;
-  const int lane = threadIdx.x % 64, m = lane % 16, q = lane / 16;
-  Rows<KP, TIn> kr, qr;
-  kr.load(static_cast<const TIn*>(p.k) + first * p.k_stride + static_cast<int64_t>(hk) * p.K, k_off,
-          static_cast<uint32_t>(p.k_stride * sizeof(TIn)), p.K, rows);
-  const bool outputs = p.o != nullptr;
-  if (outputs)
-    qr.load(static_cast<const TIn*>(p.q) + first * p.q_stride + static_cast<int64_t>(hk) * p.K, q_off,
-            static_cast<uint32_t>(p.q_stride * sizeof(TIn)), p.K, rows);
-  float g = 0.f, beta = 0.f;
-  if (lane < rows) {
-    const int64_t th = (first + lane) * p.Hv + h;
-    g = p.g != nullptr ? p.g[th] : 0.f;
-    g = g < kDeltaErase ? kDeltaErase : g;
-    beta = p.beta != nullptr ? p.beta[th] : 1.f;
+// What a prepare wave reads of a block, on its way.
+template <int KP, int OUT, typename TIn>
+struct Inputs {
+  Rows<KP, TIn> k, q;
+  float g, beta;
+  int rows;
+
+  // Block c of the sequence.
+  __device__ __forceinline__ void load(const DeltaParams& p, Span span, int c, int hk, int h, uint32_t k_off,
+                                       uint32_t q_off) {
+    const int64_t first = span.begin + static_cast<int64_t>(c) * kBlockTokens, left = span.end - first;
+    rows = left < kBlockTokens ? static_cast<int>(left) : kBlockTokens;
+    const int64_t head = static_cast<int64_t>(hk) * p.K;
+    k.load(static_cast<const TIn*>(p.k) + first * p.k_stride + head, k_off,
+           static_cast<uint32_t>(p.k_stride * sizeof(TIn)), p.K, rows);
+    if (OUT)
+      q.load(static_cast<const TIn*>(p.q) + first * p.q_stride + head, q_off,
+             static_cast<uint32_t>(p.q_stride * sizeof(TIn)), p.K, rows);
+    g = beta = 0.f;
+    const int lane = threadIdx.x % 64;
+    if (lane < rows) {
+      const int64_t th = (first + lane) * p.Hv + h;
+      if (p.g != nullptr) g = p.g[th];
+      beta = p.beta != nullptr ? p.beta[th] : 1.f;
+    }
   }
+};
+
+// A block's operands from its inputs, once the buffer is free; `next` is called
+// when the inputs' registers are.
+template <int KP, bool IN32, int OUT, typename TIn, typename Next>
+__device__ __forceinline__ void prepare_block(const DeltaParams& p, Inputs<KP, OUT, TIn>& in, Scratch& s,
+                                              Buffer<KP, IN32, OUT>& buf, const int* done, int waves, int free_at,
+                                              Next next) {
+  constexpr int kSteps = KP / 32;
+  int lane = fresh_lane();
+  constexpr bool outputs = OUT != kNoOutput;
   for (int w = 0; w < waves; ++w) wait_for(&done[w], free_at);
 
-  double b = static_cast<double>(g);
+  double b = static_cast<double>(in.g < kDeltaErase ? kDeltaErase : in.g);
 #pragma unroll
   for (int d = 1; d < kBlockTokens; d <<= 1) {
     const double up = __shfl_up(b, d, kBlockTokens);
     if (lane % kBlockTokens >= d) b += up;
   }
-  make_operand<KP, IN32, true, TIn>(kr, buf.k, buf.kt, s.rk, rows, p.norm, p.eps);
-  if (outputs) make_operand<KP, IN32, false, TIn>(qr, buf.q, buf.kt, s.rq, rows, p.norm, p.eps);
+  make_operand<KP, IN32, true, TIn>(in.k, buf.k, buf.kt, s.rk);
+  if constexpr (outputs) make_operand<KP, IN32, false, TIn>(in.q, buf.q, buf.kt, s.rq);
+  wave_fence();
+  // lane l has token l % 32 (a token behind the last one has no key and no query)
+  const bool live = lane % kBlockTokens < in.rows;
+  const float rk = live ? row_factor(s.rk[lane % kBlockTokens], p.norm, p.eps) : 0.f;
+  const float rq = live && outputs ? row_factor(s.rq[lane % kBlockTokens], p.norm, p.eps) : 0.f;
+  const double b2 = b * 1.4426950408889634;
   if (lane < kBlockTokens) {
-    s.b[lane] = b;
-    s.beta[lane] = beta;
+    s.b[lane] = static_cast<float>(b2);
+    s.b_low[lane] = static_cast<float>(b2 - static_cast<double>(s.b[lane]));
+    s.rk[lane] = rk;
+    s.beta[lane] = in.beta;
   }
+  if (!IN32) next();
   wave_fence();
 
+  lane = fresh_lane();
+  int m = lane % 16, q = lane / 16;
   // k_i.k_j and q_i.k_j with i in the lanes and j = 4 q + r in the registers
   float4v kk[3] = {}, qk[3] = {};  // tiles (0, 0), (1, 0), (1, 1)
 #pragma unroll
@@ -365,8 +420,8 @@ __device__ __forceinline__ void prepare_block(const DeltaParams& p, int hk, int 
       half8 kl[2], ql[2];
 #pragma unroll
       for (int t = 0; t < 2; ++t) {
-        kl[t] = buf.k[Buffer<KP, IN32, OUT32>::kHalves - 1][t][st][at];
-        if (outputs) ql[t] = buf.q[Buffer<KP, IN32, OUT32>::kHalves - 1][t][st][at];
+        kl[t] = buf.k[Buffer<KP, IN32, OUT>::kHalves - 1][t][st][at];
+        if (outputs) ql[t] = buf.q[Buffer<KP, IN32, OUT>::kHalves - 1][t][st][at];
       }
 #pragma unroll
       for (int i = 0; i < 3; ++i) {
@@ -379,92 +434,103 @@ __device__ __forceinline__ void prepare_block(const DeltaParams& p, int hk, int 
       }
     }
   }
+  float* const A = reinterpret_cast<float*>(&buf.t);
   float4v pm[3];
 #pragma unroll
   for (int i = 0; i < 3; ++i) {
-    const int ti = i > 0, tj = i / 2, row = 16 * ti + m;
-    const double bi = s.b[row];
-    const float ri = s.rk[row] * s.beta[row];
+    const int ti = i > 0, tj = i / 2, row = 16 * ti + m, cols = 16 * tj + 4 * q;
+    const float bi = s.b[row], bi_low = s.b_low[row], ri = s.rk[row] * s.beta[row];
+    const float4v bj = *reinterpret_cast<const float4v*>(&s.b[cols]);
+    const float4v bj_low = *reinterpret_cast<const float4v*>(&s.b_low[cols]);
+    const float4v rj = *reinterpret_cast<const float4v*>(&s.rk[cols]);
     float4v a;
 #pragma unroll
     for (int r = 0; r < 4; ++r) {
-      const int col = 16 * tj + 4 * q + r;
-      const float decay = __builtin_amdgcn_exp2f(static_cast<float>(bi - s.b[col]) * kLog2e);
-      a[r] = row > col ? ri * s.rk[col] * (decay * kk[i][r]) : 0.f;
-      pm[i][r] = row >= col ? decay * qk[i][r] : 0.f;
+      const float d = (bi - bj[r]) + (bi_low - bj_low[r]);
+      const float decay = __builtin_amdgcn_exp2f(ti > tj || row >= cols + r ? d : -__builtin_inff());
+      const float v = ri * rj[r] * (decay * kk[i][r]);
+      a[r] = ti > tj || row > cols + r ? v : 0.f;
+      pm[i][r] = decay * qk[i][r];
     }
-    *reinterpret_cast<float4v*>(&s.a[row * kAStride + 16 * tj + 4 * q]) = a;
+    *reinterpret_cast<float4v*>(&A[a_at(row, cols)]) = a;
   }
-  if (outputs) {
+  if constexpr (outputs) {
     const float4v none = {};
 #pragma unroll
     for (int t = 0; t < 2; ++t) {
       half8 hi, lo;
       split(pm[t], t ? pm[2] : none, hi, lo);
       buf.p[0][t][lane] = hi;
-      if (OUT32) buf.p[OUT32][t][lane] = lo;
+      if (OUT == kOut32) buf.p[OUT - 1][t][lane] = lo;
     }
   }
   wave_fence();
 
+  lane = fresh_lane();
+  m = lane % 16;
+  q = lane / 16;
   // (I + A)^-1 of the two diagonal 16 x 16 blocks: lane l has column l % 16 of
   // block l / 16 (the upper lanes repeat the lower ones)
   const int blk = q & 1;
   float col[16];
-  const float* diag = &s.a[16 * blk * kAStride + 16 * blk];
 #pragma unroll
   for (int i = 0; i < 16; ++i) {
     float sum = i == m ? 1.f : 0.f;
 #pragma unroll
     for (int j4 = 0; j4 < (i + 3) / 4; ++j4) {
-      const float4v a = *reinterpret_cast<const float4v*>(&diag[i * kAStride + 4 * j4]);
+      const float4v a = *reinterpret_cast<const float4v*>(&A[a_at(16 * blk + i, 16 * blk + 4 * j4)]);
 #pragma unroll
       for (int j = 0; j < 4; ++j)
         if (4 * j4 + j < i) sum -= a[j] * col[4 * j4 + j];
     }
     col[i] = sum;
+    // rows' loads are not drawn further ahead than this: they would fill the
+    // registers that the next block's inputs arrive in
+    if (i % 4 == 3) __builtin_amdgcn_sched_barrier(0);
   }
   wave_fence();
   if (lane < 32) {
 #pragma unroll
-    for (int i = 0; i < 16; ++i) s.a[(16 * blk + i) * kAStride + 16 * blk + m] = col[i];
+    for (int i = 0; i < 16; ++i) A[a_at(16 * blk + i, 16 * blk + m)] = col[i];
   }
   wave_fence();
+  lane = fresh_lane();
+  m = lane % 16;
+  q = lane / 16;
   // the lower left one: -T22 A21 T11, in fp32
   float4v y = {}, z = {};
 #pragma unroll
   for (int st = 0; st < 4; ++st)
-    y = mfma(s.a[(16 + m) * kAStride + 4 * st + q], s.a[(4 * st + q) * kAStride + m], y);
-  const float4v t22 = *reinterpret_cast<const float4v*>(&s.a[(16 + m) * kAStride + 16 + 4 * q]);
+    y = mfma(A[a_at(16 + m, 4 * st + q)], A[a_at(4 * st + q, m)], y);
+  const float4v t22 = *reinterpret_cast<const float4v*>(&A[a_at(16 + m, 16 + 4 * q)]);
 #pragma unroll
   for (int st = 0; st < 4; ++st) z = mfma(t22[st], y[st], z);
   wave_fence();
 #pragma unroll
-  for (int r = 0; r < 4; ++r) s.a[(16 + 4 * q + r) * kAStride + m] = -z[r];
+  for (int r = 0; r < 4; ++r) A[a_at(16 + 4 * q + r, m)] = -z[r];
   wave_fence();
   {
     const float4v beta0 = *reinterpret_cast<const float4v*>(&s.beta[4 * q]);
     const float4v beta1 = *reinterpret_cast<const float4v*>(&s.beta[16 + 4 * q]);
     const float4v none = {};
-    const float4v t11 = *reinterpret_cast<const float4v*>(&s.a[m * kAStride + 4 * q]) * beta0;
-    const float4v t21 = *reinterpret_cast<const float4v*>(&s.a[(16 + m) * kAStride + 4 * q]) * beta0;
+    const float4v t11 = *reinterpret_cast<const float4v*>(&A[a_at(m, 4 * q)]) * beta0;
+    const float4v t21 = *reinterpret_cast<const float4v*>(&A[a_at(16 + m, 4 * q)]) * beta0;
     const float4v tt2 = t22 * beta1;
     float most = 0.f;
 #pragma unroll
     for (int r = 0; r < 4; ++r) most = max_abs(max_abs(max_abs(most, t11[r]), t21[r]), tt2[r]);
     const Scale sc = scale_of(wave_max(most));
     half8 hi, lo;
+    wave_fence();  // A has been read
     split(t11 * sc.up, none, hi, lo);
     buf.t[0][0][lane] = hi;
     buf.t[1][0][lane] = lo;
     split(t21 * sc.up, tt2 * sc.up, hi, lo);
     buf.t[0][1][lane] = hi;
     buf.t[1][1][lane] = lo;
-    const int token = lane % kBlockTokens;
-    const double end = s.b[kBlockTokens - 1];
-    const float rk = s.rk[token], fo = outputs ? p.scale * s.rq[token] : 0.f;
-    const float eb = __builtin_amdgcn_exp2f(static_cast<float>(b) * kLog2e);
-    const float fu = rk * __builtin_amdgcn_exp2f(static_cast<float>(end - b) * kLog2e);
+    const float fo = p.scale * rq;
+    const float eb = __builtin_amdgcn_exp2f(static_cast<float>(b2));
+    const float fu = rk * __builtin_amdgcn_exp2f(static_cast<float>(readlane_d(b2, kBlockTokens - 1) - b2));
     const float largest = wave_max(fmaxf(rk, fu));
     if (lane < kBlockTokens) {
       buf.f.x[lane] = rk * eb;
@@ -480,6 +546,7 @@ __device__ __forceinline__ void prepare_block(const DeltaParams& p, int hk, int 
     }
   }
   wave_fence();
+  if (IN32) next();  // 128 registers of inputs: no room beside the rest
 }
 
 // -------------------------------------------------------------------- chain
@@ -501,6 +568,7 @@ __device__ __forceinline__ void load_cols(__amdgpu_buffer_rsrc_t r, uint32_t off
 template <typename T>
 __device__ __forceinline__ float col_value(const uint32_t (&raw)[2], int n) {
   if constexpr (sizeof(T) == 4) return __uint_as_float(raw[n]);
+  if constexpr (std::is_same_v<T, f16_t>) return widen(f16_t{static_cast<uint16_t>(raw[0] >> 16 * n)});
   return __uint_as_float(n ? raw[0] & 0xffff0000u : raw[0] << 16);
 }
 template <typename T, int NV>
@@ -512,56 +580,56 @@ __device__ __forceinline__ void store_cols(__amdgpu_buffer_rsrc_t r, uint32_t of
       __builtin_amdgcn_raw_buffer_store_b64(uint2v{__float_as_uint(v[0]), __float_as_uint(v[1])}, r, off, 0, 0);
   } else {
     if constexpr (NV == 1)
-      __builtin_amdgcn_raw_buffer_store_b16(narrow<bf16_t>(v[0]).bits, r, off, 0, 0);
+      __builtin_amdgcn_raw_buffer_store_b16(narrow<T>(v[0]).bits, r, off, 0, 0);
     else
       __builtin_amdgcn_raw_buffer_store_b32(
-          narrow<bf16_t>(v[0]).bits | static_cast<uint32_t>(narrow<bf16_t>(v[1]).bits) << 16, r, off, 0, 0);
+          narrow<T>(v[0]).bits | static_cast<uint32_t>(narrow<T>(v[1]).bits) << 16, r, off, 0, 0);
   }
 }
 
-// The states of a wave's columns: rows of tile t, register r are the state row
-// 32 (t / 2) + 8 q + 4 (t % 2) + r, columns col .. col + NV - 1.
+// The states of a wave's columns: row r of tile t is the state row 32 (t / 2) +
+// 8 q + 4 (t % 2) + r, columns col .. col + NV - 1.  Rows from K on lie past the
+// buffer's end: read as zeros, not written.
 template <int KP, int NV, typename TSt>
-__device__ __forceinline__ void load_state(const TSt* base, int64_t V, int K, int col, float4v (&S)[NV][KP / 16]) {
-  const int q = threadIdx.x % 64 / 16;
+__device__ __forceinline__ void load_state(const TSt* base, int V, int K, int col, float4v (&S)[NV][KP / 16]) {
+  constexpr uint32_t kSize = sizeof(TSt);
+  const __amdgpu_buffer_rsrc_t buf = make_rsrc(base, static_cast<uint32_t>(K * V) * kSize);
+  const uint32_t at = col < V ? static_cast<uint32_t>(threadIdx.x % 64 / 16 * 8 * V + col) * kSize : kDropOffset;
 #pragma unroll
   for (int t = 0; t < KP / 16; ++t) {
 #pragma unroll
     for (int r = 0; r < 4; ++r) {
-      const int row = 32 * (t / 2) + 8 * q + 4 * (t % 2) + r;
-      if (row < K && col < V) {
-        const Pack<TSt, NV> v = load_pack<NV>(base + row * V + col);
+      uint32_t raw[2];
+      load_cols<TSt, NV>(buf, at + static_cast<uint32_t>((32 * (t / 2) + 4 * (t % 2) + r) * V) * kSize, raw);
 #pragma unroll
-        for (int n = 0; n < NV; ++n) S[n][t][r] = widen(v.v[n]);
-      }
+      for (int n = 0; n < NV; ++n) S[n][t][r] = col_value<TSt>(raw, n);
     }
   }
 }
 template <int KP, int NV, typename TSt>
-__device__ __forceinline__ void store_state(TSt* base, int64_t V, int K, int col, const float4v (&S)[NV][KP / 16]) {
-  const int q = threadIdx.x % 64 / 16;
+__device__ __forceinline__ void store_state(TSt* base, int V, int K, int col, const float4v (&S)[NV][KP / 16]) {
+  constexpr uint32_t kSize = sizeof(TSt);
+  const __amdgpu_buffer_rsrc_t buf = make_rsrc(base, static_cast<uint32_t>(K * V) * kSize);
+  const uint32_t at = col < V ? static_cast<uint32_t>(threadIdx.x % 64 / 16 * 8 * V + col) * kSize : kDropOffset;
 #pragma unroll
   for (int t = 0; t < KP / 16; ++t) {
 #pragma unroll
     for (int r = 0; r < 4; ++r) {
-      const int row = 32 * (t / 2) + 8 * q + 4 * (t % 2) + r;
-      if (row < K && col < V) {
-        float v[NV];
+      float v[NV];
 #pragma unroll
-        for (int n = 0; n < NV; ++n) v[n] = S[n][t][r];
-        store_pack<NV>(base + row * V + col, v);
-      }
+      for (int n = 0; n < NV; ++n) v[n] = S[n][t][r];
+      store_cols<TSt, NV>(buf, at + static_cast<uint32_t>((32 * (t / 2) + 4 * (t % 2) + r) * V) * kSize, v);
     }
   }
 }
 
-template <int KP, bool IN32, bool OUT32, int NV>
-__global__ void __launch_bounds__(64 * (kChainMax + Shared<KP, IN32, OUT32>::kPrepare))
+template <int KP, bool IN32, int OUT, int NV>
+__global__ void __launch_bounds__(64 * (kChainMax + Shared<KP, IN32, OUT>::kPrepare))
     delta_kernel(DeltaParams p, int chain_waves, int state16) {
   using TIn = std::conditional_t<IN32, float, bf16_t>;
-  using TOut = std::conditional_t<OUT32, float, bf16_t>;
-  using Sh = Shared<KP, IN32, OUT32>;
-  using Buf = Buffer<KP, IN32, OUT32>;
+  using TOut = std::conditional_t<OUT == kOut32, float, bf16_t>;
+  using Sh = Shared<KP, IN32, OUT>;
+  using Buf = Buffer<KP, IN32, OUT>;
   constexpr int kSteps = KP / 32, kTiles = KP / 16, kLow = Buf::kHalves - 1;
   static_assert(sizeof(Sh) <= 160 * 1024, "LDS of a CU");
   __shared__ __align__(16) unsigned char lds[sizeof(Sh)];
@@ -588,12 +656,14 @@ __global__ void __launch_bounds__(64 * (kChainMax + Shared<KP, IN32, OUT32>::kPr
     const int self = wave - chain_waves;
     const uint32_t k_off = Rows<KP, TIn>::lane_offset(static_cast<uint32_t>(p.k_stride * sizeof(TIn)), p.K);
     const uint32_t q_off = Rows<KP, TIn>::lane_offset(static_cast<uint32_t>(p.q_stride * sizeof(TIn)), p.K);
+    Inputs<KP, OUT, TIn> in;
+    if (self < blocks) in.load(p, span, self, hk, h, k_off, q_off);
     for (int c = self; c < blocks; c += Sh::kPrepare) {
-      const int64_t first = span.begin + static_cast<int64_t>(c) * kBlockTokens;
-      const int64_t left = span.end - first;
-      const int rows = left < kBlockTokens ? static_cast<int>(left) : kBlockTokens;
-      prepare_block<KP, IN32, OUT32, TIn>(p, hk, h, k_off, q_off, first, rows, sh.scratch[self], sh.buf[c % Sh::kBuffers], sh.done,
-                                          chain_waves, c - Sh::kBuffers + 1);
+      prepare_block<KP, IN32, OUT, TIn>(p, in, sh.scratch[self], sh.buf[c % Sh::kBuffers], sh.done, chain_waves,
+                                          c - Sh::kBuffers + 1, [&] {
+                                            if (c + Sh::kPrepare < blocks)
+                                              in.load(p, span, c + Sh::kPrepare, hk, h, k_off, q_off);
+                                          });
       publish(&sh.ready[c % Sh::kBuffers], c + 1);
     }
     return;
@@ -627,7 +697,6 @@ __global__ void __launch_bounds__(64 * (kChainMax + Shared<KP, IN32, OUT32>::kPr
     }
   }
 
-  const bool outputs = p.o != nullptr;
   const uint32_t v_step = static_cast<uint32_t>(p.v_stride * sizeof(TIn));
   const uint32_t o_step = static_cast<uint32_t>(static_cast<int64_t>(p.Hv) * p.V * sizeof(TOut));
   const uint32_t v_off = col < p.V ? static_cast<uint32_t>(col * sizeof(TIn)) + 4 * q * v_step : kDropOffset;
@@ -702,14 +771,14 @@ __global__ void __launch_bounds__(64 * (kChainMax + Shared<KP, IN32, OUT32>::kPr
 #pragma unroll
           for (int n = 0; n < NV; ++n) ks[t][n] = mfma(kl, s_hi[n][st], ks[t][n]);
         }
-        if (outputs) {
+        if (OUT) {
           const half8 qf = buf.q[0][t][st][at];
 #pragma unroll
           for (int n = 0; n < NV; ++n) {
             qs[t][n] = mfma(qf, s_hi[n][st], qs[t][n]);
-            if (OUT32) qs[t][n] = mfma(qf, s_lo[n][st], qs[t][n]);
+            if (OUT == kOut32) qs[t][n] = mfma(qf, s_lo[n][st], qs[t][n]);
           }
-          if (IN32 && OUT32) {
+          if (IN32 && OUT == kOut32) {
             const half8 ql = buf.q[kLow][t][st][at];
 #pragma unroll
             for (int n = 0; n < NV; ++n) qs[t][n] = mfma(ql, s_hi[n][st], qs[t][n]);
@@ -786,13 +855,13 @@ __global__ void __launch_bounds__(64 * (kChainMax + Shared<KP, IN32, OUT32>::kPr
         u[0][n] *= unit;
         u[1][n] *= unit;
         split(u[0][n] * fu[0], u[1][n] * fu[1], u_hi[n], u_lo[n]);
-        if (OUT32)
+        if (OUT == kOut32)
           split(u[0][n] * fr[0], u[1][n] * fr[1], w_hi[n], w_lo[n]);
-        else
+        else if (OUT == kOut16)
           w_hi[n] = high(u[0][n] * fr[0], u[1][n] * fr[1]);
       }
     }
-    if (outputs) {
+    if (OUT) {
       const uint32_t rows = left < kBlockTokens ? static_cast<uint32_t>(left) : kBlockTokens;
       const __amdgpu_buffer_rsrc_t ro =
           make_rsrc(static_cast<TOut*>(p.o) + (first * p.Hv + h) * p.V,
@@ -804,9 +873,9 @@ __global__ void __launch_bounds__(64 * (kChainMax + Shared<KP, IN32, OUT32>::kPr
 #pragma unroll
         for (int n = 0; n < NV; ++n) {
           pu[n] = mfma(pf, w_hi[n], pu[n]);
-          if (OUT32) {
+          if (OUT == kOut32) {
             pu[n] = mfma(pf, w_lo[n], pu[n]);
-            pu[n] = mfma(buf.p[OUT32][t][lane], w_hi[n], pu[n]);
+            pu[n] = mfma(buf.p[OUT - 1][t][lane], w_hi[n], pu[n]);
           }
         }
         const float4v fq = *reinterpret_cast<const float4v*>(&buf.f.q[16 * t + 4 * q]);
@@ -853,12 +922,12 @@ __global__ void __launch_bounds__(64 * (kChainMax + Shared<KP, IN32, OUT32>::kPr
   }
 }
 
-template <int KP, bool IN32, bool OUT32, int NV>
+template <int KP, bool IN32, int OUT, int NV>
 hipError_t launch_typed(const DeltaParams& p, int chain_waves, int state16, hipStream_t s) {
-  using Sh = Shared<KP, IN32, OUT32>;
+  using Sh = Shared<KP, IN32, OUT>;
   const int width = 16 * NV * chain_waves;
   const int64_t grid = p.B * p.Hv * ((p.V + width - 1) / width);
-  delta_kernel<KP, IN32, OUT32, NV>
+  delta_kernel<KP, IN32, OUT, NV>
       <<<dim3(static_cast<uint32_t>(grid)), 64 * (chain_waves + Sh::kPrepare), 0, s>>>(p, chain_waves, state16);
   return hipGetLastError();
 }
@@ -875,20 +944,22 @@ hipError_t launch_delta(const DeltaParams& p, int in_dtype, int out_dtype, int s
     if (p.B * p.Hv * ((p.V + 31) / 32) < cus) nv = 1;
   }
   const int state16 = state_dtype == PRECOG_F16;
-  const auto go = [&](auto kp, auto in32, auto out32) {
-    constexpr int KP = decltype(kp)::value;
-    constexpr bool IN32 = decltype(in32)::value, OUT32 = decltype(out32)::value;
-    return nv == 2 ? launch_typed<KP, IN32, OUT32, 2>(p, waves, state16, s)
-                   : launch_typed<KP, IN32, OUT32, 1>(p, waves, state16, s);
+  const auto go = [&](auto kp, auto in32, auto out) {
+    constexpr int KP = decltype(kp)::value, OUT = decltype(out)::value;
+    constexpr bool IN32 = decltype(in32)::value;
+    return nv == 2 ? launch_typed<KP, IN32, OUT, 2>(p, waves, state16, s)
+                   : launch_typed<KP, IN32, OUT, 1>(p, waves, state16, s);
   };
-  const auto sized = [&](auto in32, auto out32) {
-    return p.K <= 64 ? go(std::integral_constant<int, 64>{}, in32, out32)
-                     : go(std::integral_constant<int, 128>{}, in32, out32);
+  const auto sized = [&](auto in32, auto out) {
+    return p.K <= 64 ? go(std::integral_constant<int, 64>{}, in32, out)
+                     : go(std::integral_constant<int, 128>{}, in32, out);
   };
-  using Yes = std::true_type;
-  using No = std::false_type;
-  if (in_dtype == PRECOG_F32) return out_dtype == PRECOG_F32 ? sized(Yes{}, Yes{}) : sized(Yes{}, No{});
-  return out_dtype == PRECOG_F32 ? sized(No{}, Yes{}) : sized(No{}, No{});
+  const auto typed = [&](auto in32) {
+    if (p.o == nullptr) return sized(in32, std::integral_constant<int, kNoOutput>{});
+    return out_dtype == PRECOG_F32 ? sized(in32, std::integral_constant<int, kOut32>{})
+                                   : sized(in32, std::integral_constant<int, kOut16>{});
+  };
+  return in_dtype == PRECOG_F32 ? typed(std::true_type{}) : typed(std::false_type{});
 }
 
 }  // namespace precog

@@ -28,10 +28,11 @@ def delta_bar(tokens):
 
 
 # What a bf16 o may have more than delta_bar, against its rms: its two terms Q S
-# and Q K^T U take operands of 11 bits (errors of at most 2^-12 each, 2^-12 / sqrt(3)
-# rms: S in the one, two in the other), together 2^-12 of the terms' rms, which are
-# up to 1.5 times o's where they partly cancel; five times that is 2^-9.1.
-O16 = 2.0 ** -9
+# and Q K^T U take operands of 11 bits, rounded by at most 2^-11 (half a step of
+# 2^-10), 2^-11 / sqrt(3) rms: S in the one, two of them in the other, together
+# 2^-11 of the terms' rms, which are up to 1.5 times o's where they partly cancel;
+# five times that is 2^-8.1.
+O16 = 2.0 ** -8
 
 
 def check(got, ref, bar, what=""):
