@@ -30,8 +30,9 @@
 //
 // Numbers.  The states, all sums, decays and norms are fp32 (b is summed in
 // fp64, where the differences of two positions are taken).  A product's
-// operands are fp16: keys and queries as 2^e times unit size (exact for bf16
-// up to 2^-30 of the row's norm; fp32 inputs as two halves of 11 bits), and S,
+// operands are fp16: keys and queries under the power of two that brings the
+// row's norm to [1, 2) (exact for bf16 down to 2^-16 of it, good to 2^-25; fp32
+// inputs as two halves of 11 bits), and S,
 // X, U and T as two halves (22 bits) under a power of two that puts their
 // column's (T: block's) largest at 2^14, so neither half runs out of range.
 // Products of two low halves are left out (2^-22).  What only enters a bf16 o
@@ -65,7 +66,7 @@ struct Factors {
   float o[kBlockTokens];   // scale |q| of Q K^T U
   float decay;             // e^{b_end}
   float t;                 // power of two that T's operand lacks
-  float most;              // largest of r and u
+  float most;              // bound of r U and u U for |X| <= 1
   float pad;
 };
 
@@ -273,12 +274,12 @@ struct Rows {
   }
 };
 
-// A row's power of two: its norm times `up` is in [2^6, 2^7).
+// A row's power of two: its norm times `up` is in [1, 2).
 __device__ __forceinline__ Scale row_scale(float sq) {
   int half_e = static_cast<int>(__float_as_uint(sq) >> 24 & 127);
-  half_e = half_e < 8 ? 8 : half_e;
-  return {__uint_as_float(static_cast<uint32_t>(127 + 63 + 6 - half_e) << 23),
-          __uint_as_float(static_cast<uint32_t>(127 - 63 - 6 + half_e) << 23)};
+  half_e = half_e < 1 ? 1 : half_e;
+  return {__uint_as_float(static_cast<uint32_t>(127 + 63 - half_e) << 23),
+          __uint_as_float(static_cast<uint32_t>(127 - 63 + half_e) << 23)};
 }
 // What a row's operand lacks: that power of two, over the norm where the row is
 // to be normalised.
@@ -519,7 +520,8 @@ __device__ __forceinline__ void prepare_block(const DeltaParams& p, Inputs<KP, O
     float most = 0.f;
 #pragma unroll
     for (int r = 0; r < 4; ++r) most = max_abs(max_abs(max_abs(most, t11[r]), t21[r]), tt2[r]);
-    const Scale sc = scale_of(wave_max(most));
+    const float t_most = wave_max(most);
+    const Scale sc = scale_of(t_most);
     half8 hi, lo;
     wave_fence();  // A has been read
     split(t11 * sc.up, none, hi, lo);
@@ -541,7 +543,7 @@ __device__ __forceinline__ void prepare_block(const DeltaParams& p, Inputs<KP, O
       if (lane == kBlockTokens - 1) buf.f.decay = eb;
       if (lane == 0) {
         buf.f.t = sc.down;
-        buf.f.most = largest;
+        buf.f.most = kBlockTokens * t_most * largest;
       }
     }
   }
@@ -718,11 +720,12 @@ __global__ void __launch_bounds__(64 * (kChainMax + Shared<KP, IN32, OUT>::kPrep
   // A column of S is held as S~ = S / sigma, sigma a power of two such that
   // |S~| < 2^16: its halves are fp16 numbers as they are.  `bound` >= |S~|.
   // A block multiplies S~ by decay sigma / sigma' and adds K^T (U / sigma'),
-  // where 32 keys' elements of at most 2^7 meet |U / sigma'| < 2^2: sigma' is
-  // chosen so that both terms stay below 2^14.  The halves' floor of 2^-24
-  // leaves them 22 bits of the column's largest while it is above 2^-2, and the
-  // bound, which is some 2^6 above it and can grow by 2^14 a block, is taken
-  // anew from S~ every eighth block.
+  // where 32 keys' elements of at most 2 meet |U / sigma'| < 2^8: sigma' is
+  // chosen so that both terms stay below 2^14, from bounds that are known before
+  // U is (|U| <= 32 |T| |X|).  The halves' floor of 2^-24 leaves them 22 bits of
+  // the column's largest while that is above 2^-2; U's bound is some 2^7 above
+  // it, and that of S~, which can grow by 2^14 a block, is taken anew from S~
+  // every eighth block.
   float sigma[NV], bound[NV];
   const auto largest = [&](int n) {
     float most = 0.f;
@@ -753,11 +756,11 @@ __global__ void __launch_bounds__(64 * (kChainMax + Shared<KP, IN32, OUT>::kPrep
     const Buf& buf = sh.buf[c % Sh::kBuffers];
     wait_for(&sh.ready[c % Sh::kBuffers], c + 1);
 
-    // K S and Q S
+    // K S, which the rest waits for, then Q S
+    const int at = q * 16 + (m ^ 4 * q);
     float4v ks[2][NV] = {}, qs[2][NV] = {};
 #pragma unroll
     for (int st = 0; st < kSteps; ++st) {
-      const int at = q * 16 + (m ^ 4 * q);
 #pragma unroll
       for (int t = 0; t < 2; ++t) {
         const half8 kf = buf.k[0][t][st][at];
@@ -771,7 +774,14 @@ __global__ void __launch_bounds__(64 * (kChainMax + Shared<KP, IN32, OUT>::kPrep
 #pragma unroll
           for (int n = 0; n < NV; ++n) ks[t][n] = mfma(kl, s_hi[n][st], ks[t][n]);
         }
-        if (OUT) {
+      }
+    }
+    __builtin_amdgcn_sched_barrier(0);
+    if (OUT) {
+#pragma unroll
+      for (int st = 0; st < kSteps; ++st) {
+#pragma unroll
+        for (int t = 0; t < 2; ++t) {
           const half8 qf = buf.q[0][t][st][at];
 #pragma unroll
           for (int n = 0; n < NV; ++n) {
@@ -788,7 +798,7 @@ __global__ void __launch_bounds__(64 * (kChainMax + Shared<KP, IN32, OUT>::kPrep
     }
     // X, then U = T X without the powers of two of their operands
     float4v u[2][NV] = {};
-    float u_unit[NV];
+    float u_unit[NV], u_most[NV];
     {
       float4v x[2][NV];
 #pragma unroll
@@ -808,8 +818,10 @@ __global__ void __launch_bounds__(64 * (kChainMax + Shared<KP, IN32, OUT>::kPrep
         for (int t = 0; t < 2; ++t)
 #pragma unroll
           for (int r = 0; r < 4; ++r) most = max_abs(most, x[t][n][r]);
-        const Scale sc = scale_of(max_of_rows(most));
+        most = max_of_rows(most);
+        const Scale sc = scale_of(most);
         u_unit[n] = sc.down * buf.f.t;
+        u_most[n] = most * buf.f.most;
         split(x[0][n] * sc.up, x[1][n] * sc.up, x_hi[n], x_lo[n]);
       }
 #pragma unroll
@@ -833,24 +845,18 @@ __global__ void __launch_bounds__(64 * (kChainMax + Shared<KP, IN32, OUT>::kPrep
         fr[t] = *reinterpret_cast<const float4v*>(&buf.f.r[16 * t + 4 * q]);
         fu[t] = *reinterpret_cast<const float4v*>(&buf.f.u[16 * t + 4 * q]);
       }
-      const float f_most = buf.f.most, decay = buf.f.decay;
+      const float decay = buf.f.decay;
 #pragma unroll
       for (int n = 0; n < NV; ++n) {
-        float most = 0.f;
-#pragma unroll
-        for (int t = 0; t < 2; ++t)
-#pragma unroll
-          for (int r = 0; r < 4; ++r) most = max_abs(most, u[t][n][r]);
-        most = max_of_rows(most) * f_most * u_unit[n];
         // the last term bounds sigma / sigma' by 2^64 where S and U vanish
-        int e = exponent(most) - 1;
+        int e = exponent(u_most[n]) - 7;
         e = max(e, exponent(bound[n] * sigma[n] * decay) - 13);
         e = max(e, exponent(sigma[n]) - 64);
         e = min(max(e, 2), 252);
         next[n] = __uint_as_float(static_cast<uint32_t>(e) << 23);
         const float up = __uint_as_float(static_cast<uint32_t>(254 - e) << 23);
         keep[n] = sigma[n] * up * decay;
-        bound[n] = bound[n] * keep[n] + 4096.f * (most * up);
+        bound[n] = bound[n] * keep[n] + 64.f * (u_most[n] * up);
         const float unit = u_unit[n] * up;
         u[0][n] *= unit;
         u[1][n] *= unit;
@@ -859,6 +865,17 @@ __global__ void __launch_bounds__(64 * (kChainMax + Shared<KP, IN32, OUT>::kPrep
           split(u[0][n] * fr[0], u[1][n] * fr[1], w_hi[n], w_lo[n]);
         else if (OUT == kOut16)
           w_hi[n] = high(u[0][n] * fr[0], u[1][n] * fr[1]);
+      }
+    }
+#pragma unroll
+    for (int t = 0; t < kTiles; ++t) {
+      const half8 kf = buf.kt[0][t][lane];
+#pragma unroll
+      for (int n = 0; n < NV; ++n) {
+        S[n][t] *= keep[n];
+        S[n][t] = mfma(kf, u_hi[n], S[n][t]);
+        S[n][t] = mfma(kf, u_lo[n], S[n][t]);
+        if (IN32) S[n][t] = mfma(buf.kt[kLow][t][lane], u_hi[n], S[n][t]);
       }
     }
     if (OUT) {
@@ -888,17 +905,6 @@ __global__ void __launch_bounds__(64 * (kChainMax + Shared<KP, IN32, OUT>::kPrep
             v[n] = fq[r] * (sigma[n] * qs[t][n][r]) + fo[r] * (next[n] * pu[n][r]);
           store_cols<TOut, NV>(ro, o_off + (16 * t + r) * o_step, v);
         }
-      }
-    }
-#pragma unroll
-    for (int t = 0; t < kTiles; ++t) {
-      const half8 kf = buf.kt[0][t][lane];
-#pragma unroll
-      for (int n = 0; n < NV; ++n) {
-        S[n][t] *= keep[n];
-        S[n][t] = mfma(kf, u_hi[n], S[n][t]);
-        S[n][t] = mfma(kf, u_lo[n], S[n][t]);
-        if (IN32) S[n][t] = mfma(buf.kt[kLow][t][lane], u_hi[n], S[n][t]);
       }
     }
 #pragma unroll
