@@ -159,6 +159,17 @@ __device__ __forceinline__ Scale scale_of(float m) {
   return {__uint_as_float(static_cast<uint32_t>(268 - e) << 23), __uint_as_float(static_cast<uint32_t>(e - 14) << 23)};
 }
 
+// x - h[i], in one instruction.
+template <int I>
+__device__ __forceinline__ float less_half(float x, half2 h) {
+  float d;
+  if constexpr (I == 0)
+    asm("v_fma_mix_f32 %0, %1, -1.0, %2 op_sel_hi:[1,0,0]" : "=v"(d) : "v"(h), "v"(x));
+  else
+    asm("v_fma_mix_f32 %0, %1, -1.0, %2 op_sel:[1,0,0] op_sel_hi:[1,0,0]" : "=v"(d) : "v"(h), "v"(x));
+  return d;
+}
+
 // Eight fp32 values as halves of 11 bits each, or as the high ones alone.
 __device__ __forceinline__ void split(const float4v& a, const float4v& b, half8& hi, half8& lo) {
   half2 h[4], l[4];
@@ -166,7 +177,7 @@ __device__ __forceinline__ void split(const float4v& a, const float4v& b, half8&
   for (int i = 0; i < 4; ++i) {
     const float x = i < 2 ? a[2 * i] : b[2 * i - 4], y = i < 2 ? a[2 * i + 1] : b[2 * i - 3];
     h[i] = to_half2(x, y);
-    l[i] = to_half2(x - static_cast<float>(h[i][0]), y - static_cast<float>(h[i][1]));
+    l[i] = to_half2(less_half<0>(x, h[i]), less_half<1>(y, h[i]));
   }
   hi = half8{h[0][0], h[0][1], h[1][0], h[1][1], h[2][0], h[2][1], h[3][0], h[3][1]};
   lo = half8{l[0][0], l[0][1], l[1][0], l[1][1], l[2][0], l[2][1], l[3][0], l[3][1]};
@@ -310,7 +321,7 @@ __device__ __forceinline__ void make_operand(const Rows<KP, TIn>& rows, Frags& f
       word[0][j] = __builtin_bit_cast(uint32_t, h);
       if (IN32)
         word[1][j] = __builtin_bit_cast(
-            uint32_t, to_half2(x - static_cast<float>(h[0]), y - static_cast<float>(h[1])));
+            uint32_t, to_half2(less_half<0>(x, h), less_half<1>(y, h)));
     }
     const int tile = lp / 4, m = 4 * (lp % 4) + row, q = c % 4;
 #pragma unroll
@@ -704,12 +715,17 @@ __global__ void __launch_bounds__(64 * (kChainMax + Shared<KP, IN32, OUT>::kPrep
   const uint32_t v_off = col < p.V ? static_cast<uint32_t>(col * sizeof(TIn)) + 4 * q * v_step : kDropOffset;
   const uint32_t o_off = col < p.V ? static_cast<uint32_t>(col * sizeof(TOut)) + 4 * q * o_step : kDropOffset;
   uint32_t raw[2][4][2];  // the block's values: tokens 16 t + 4 q + r
+  const int tokens = static_cast<int>(span.end - span.begin);
+  const TIn* v_at = static_cast<const TIn*>(p.v) + span.begin * p.v_stride + static_cast<int64_t>(h) * p.V;
+  TOut* o_at = static_cast<TOut*>(p.o) + (span.begin * p.Hv + h) * p.V;
+  // rows of block c
+  const auto rows_of = [&](int c) {
+    return static_cast<uint32_t>(min(tokens - c * kBlockTokens, kBlockTokens));
+  };
   const auto fetch = [&](int c) {
-    const int64_t first = span.begin + static_cast<int64_t>(c) * kBlockTokens, left = span.end - first;
-    const uint32_t rows = left < kBlockTokens ? static_cast<uint32_t>(left) : kBlockTokens;
     const __amdgpu_buffer_rsrc_t r =
-        make_rsrc(static_cast<const TIn*>(p.v) + first * p.v_stride + static_cast<int64_t>(h) * p.V,
-                  (rows - 1) * v_step + p.V * static_cast<uint32_t>(sizeof(TIn)));
+        make_rsrc(v_at, (rows_of(c) - 1) * v_step + p.V * static_cast<uint32_t>(sizeof(TIn)));
+    v_at += kBlockTokens * p.v_stride;
 #pragma unroll
     for (int t = 0; t < 2; ++t)
 #pragma unroll
@@ -746,7 +762,6 @@ __global__ void __launch_bounds__(64 * (kChainMax + Shared<KP, IN32, OUT>::kPrep
   }
 
   for (int c = 0; c < blocks; ++c) {
-    const int64_t first = span.begin + static_cast<int64_t>(c) * kBlockTokens, left = span.end - first;
     // the state as an operand
     half8 s_hi[NV][kSteps], s_lo[NV][kSteps];
 #pragma unroll
@@ -879,10 +894,9 @@ __global__ void __launch_bounds__(64 * (kChainMax + Shared<KP, IN32, OUT>::kPrep
       }
     }
     if (OUT) {
-      const uint32_t rows = left < kBlockTokens ? static_cast<uint32_t>(left) : kBlockTokens;
       const __amdgpu_buffer_rsrc_t ro =
-          make_rsrc(static_cast<TOut*>(p.o) + (first * p.Hv + h) * p.V,
-                    (rows - 1) * o_step + p.V * static_cast<uint32_t>(sizeof(TOut)));
+          make_rsrc(o_at, (rows_of(c) - 1) * o_step + p.V * static_cast<uint32_t>(sizeof(TOut)));
+      o_at += static_cast<int64_t>(kBlockTokens) * p.Hv * p.V;
 #pragma unroll
       for (int t = 0; t < 2; ++t) {
         const half8 pf = buf.p[0][t][lane];
