@@ -677,7 +677,7 @@ size_t precog_score_workspace_bytes(int64_t T, int64_t V, int64_t top);
  * nothing unmasked has logprob -infinity and entropy 0.  A row with a NaN or a
  * +infinity has NaN in all its numbers and ids of -1.  Sums in fp32.
  *   workspace  precog_score_workspace_bytes(T, V, top) bytes
- * T, V < 2^31; logits aligned as their type, workspace 16 bytes, others 4. */
+ * T < 2^31, V <= 2^28; logits aligned as their type, workspace 16 bytes, others 4. */
 precog_status precog_score_tokens(const void *logits, precog_dtype logits_dtype,
                                   int64_t T, int64_t V, int64_t row_stride,
                                   const int32_t *token, int64_t top,

@@ -122,12 +122,6 @@ __device__ __forceinline__ half2 to_half2(float a, float b) {
   return __builtin_convertvector((float2v{a, b}), half2);  // nearest even
 }
 
-// Orders a wave's LDS accesses before and after it (other lanes' among them).
-__device__ __forceinline__ void wave_fence() {
-  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-  __builtin_amdgcn_wave_barrier();
-}
-
 // The lane's number as a value of its own: what is computed from it is not kept
 // in registers from one part of a long function to the next.
 __device__ __forceinline__ int fresh_lane() {

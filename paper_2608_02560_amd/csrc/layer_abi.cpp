@@ -124,7 +124,7 @@ int64_t score_splits(int64_t T, int64_t V) {
 }
 
 bool valid_score(int64_t T, int64_t V, int64_t top) {
-  return T >= 0 && V >= 1 && T <= 0x7fffffffLL && V <= 0x7fffffffLL && top >= 0 &&
+  return T >= 0 && V >= 1 && T <= 0x7fffffffLL && V <= (1LL << 28) && top >= 0 &&
          top <= precog::kScoreMaxTop;
 }
 

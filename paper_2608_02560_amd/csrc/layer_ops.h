@@ -42,6 +42,12 @@ __device__ __forceinline__ void store_pack(T* at, const float (&f)[N]) {
   *reinterpret_cast<Pack<T, N>*>(at) = r;
 }
 
+// Orders a wave's LDS accesses before and after it (other lanes' among them).
+__device__ __forceinline__ void wave_fence() {
+  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+  __builtin_amdgcn_wave_barrier();
+}
+
 // Begin and end of sequence b among T tokens: [b * L, (b + 1) * L), or the
 // clamped [starts[b], starts[b + 1]); an end before its begin is empty.
 struct Span {

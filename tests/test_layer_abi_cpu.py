@@ -133,7 +133,7 @@ def test_conv_arguments():
 
 def test_score_arguments():
     assert _score(T=-1) == ESHAPE and _score(V=0) == ESHAPE and _score(top=65) == ESHAPE and _score(top=-1) == ESHAPE
-    assert _score(T=1 << 31) == ESHAPE and _score(V=1 << 31) == ESHAPE
+    assert _score(T=1 << 31) == ESHAPE and _score(V=(1 << 28) + 1) == ESHAPE
     assert _score(dtype=5) == EDTYPE
     assert _score(stride=999) == ESTRIDE
     for name in ("logits", "lp", "ids", "tlp"):
