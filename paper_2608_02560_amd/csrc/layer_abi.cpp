@@ -112,13 +112,15 @@ precog::ConvParams conv_params(const precog_conv_desc* d, const void* x, const f
   return p;
 }
 
-// Workgroups of one row of a scoring call: one when the rows alone give each
-// of the 256 CUs eight workgroups, else as many as bring the call there while
-// each keeps two tiles to read.
+// Workgroups of one row of a scoring call: as many as give each of the 256 CUs
+// one (more of them cost more than they read faster: 333 rows of 32,003 fp32
+// logits take 17.4 us with one a CU, 20.5 us with two, 28.6 us with eight), each
+// with four tiles or more, which its waves load at once (8 rows of 131,072 bf16
+// logits: 12.7 us; with two tiles each 15.4 us).
 int64_t score_splits(int64_t T, int64_t V) {
   const int64_t tiles = (V + precog::kScoreTile - 1) / precog::kScoreTile;
-  const int64_t want = (8 * 256 + T - 1) / T;
-  const int64_t most = tiles / 2 < 64 ? tiles / 2 : 64;
+  const int64_t want = (256 + T - 1) / T;
+  const int64_t most = tiles / 4 < 64 ? tiles / 4 : 64;
   const int64_t n = want < most ? want : most;
   return n < 1 ? 1 : n;
 }

@@ -68,11 +68,32 @@ struct Entry {
   int id;
 };
 
+// The value of lane l ^ kMask, without a trip through LDS.
+template <int kMask>
+__device__ __forceinline__ int other_lane(int v) {
+  constexpr int kHalfMirror = 0x141, kQuadMirror = 0x1B;  // l ^ 7, l ^ 3
+  if constexpr (kMask == 1) return dpp<kQuadSwap1>(v);
+  if constexpr (kMask == 2) return dpp<kQuadSwap2>(v);
+  if constexpr (kMask == 4) return dpp<kQuadMirror>(dpp<kHalfMirror>(v));
+  if constexpr (kMask == 8) return dpp<kRowRor8>(v);
+  const bool upper = threadIdx.x % 64 & kMask;
+  if constexpr (kMask == 16) {
+    const auto s = __builtin_amdgcn_permlane16_swap(v, v, false, false);
+    return upper ? s[0] : s[1];
+  }
+  const auto s = __builtin_amdgcn_permlane32_swap(v, v, false, false);
+  return upper ? s[0] : s[1];
+}
+template <int kMask>
+__device__ __forceinline__ Entry other_lane(const Entry& e) {
+  return {__int_as_float(other_lane<kMask>(__float_as_int(e.val))), other_lane<kMask>(e.id)};
+}
+
 // One stage of a bitonic network: lanes l and l ^ kMask keep the better or the
 // worse of their entries.
 template <int kMask>
 __device__ __forceinline__ void exchange(Entry& e, bool keep_better) {
-  const Entry o{__shfl_xor(e.val, kMask), __shfl_xor(e.id, kMask)};
+  const Entry o = other_lane<kMask>(e);
   if (better(o.val, o.id, e.val, e.id) == keep_better) e = o;
 }
 
@@ -98,7 +119,9 @@ __device__ __forceinline__ void sort64(Entry& e) {
 // The best 64 of two sorted lists, sorted.
 __device__ __forceinline__ void merge64(Entry& list, const Entry& other) {
   const int lane = threadIdx.x % 64;
-  const Entry o{__shfl_xor(other.val, 63), __shfl_xor(other.id, 63)};
+  constexpr int kRowMirror = 0x140;  // l ^ 15
+  Entry o{dpp<kRowMirror>(other.val), dpp<kRowMirror>(other.id)};
+  o = other_lane<32>(other_lane<16>(o));
   if (better(o.val, o.id, list.val, list.id)) list = o;
   const auto stage = [&](auto mask) {
     exchange<decltype(mask)::value>(list, (lane & decltype(mask)::value) == 0);
@@ -168,9 +191,6 @@ __global__ void __launch_bounds__(kThreads) score_kernel(ScoreParams p) {
   // 16-byte aligned address at or below the row; its logits begin `skip` on
   const uintptr_t at = reinterpret_cast<uintptr_t>(p.logits) + row * p.row_stride * sizeof(T);
   const int skip = static_cast<int>((at & 15) / sizeof(T));
-  const __amdgpu_buffer_rsrc_t base =
-      make_rsrc(reinterpret_cast<const void*>(at & ~static_cast<uintptr_t>(15)),
-                static_cast<uint32_t>((skip + p.V) * sizeof(T) + 3) & ~3u);
 
   Sums a{kNone, 0.f, 0.f};
   Entry best{kNone, -1};
@@ -194,6 +214,10 @@ __global__ void __launch_bounds__(kThreads) score_kernel(ScoreParams p) {
   const int begin = part * span;
   const int low = part == 0 ? skip : begin;
   const int high = begin >= vocab ? low : begin + span >= vocab ? vocab + skip : begin + span;
+  // loads past the last position read nothing
+  const __amdgpu_buffer_rsrc_t base =
+      make_rsrc(reinterpret_cast<const void*>(at & ~static_cast<uintptr_t>(15)),
+                (static_cast<uint32_t>(high) * sizeof(T) + 3) & ~3u);
   struct Group {
     uint4v raw[kTiles][sizeof(T) * kLane / 16];
   };
@@ -314,15 +338,38 @@ __global__ void __launch_bounds__(kThreads) score_kernel(ScoreParams p) {
   }
 }
 
-// Joins the parts of a row: one wave, one part a lane.  Each round takes the
-// best head of the parts' sorted lists.
-template <typename T>
-__global__ void __launch_bounds__(64) score_join_kernel(ScoreParams p) {
-  const int lane = threadIdx.x;
-  const int64_t row = blockIdx.x, piece = row * p.splits + lane;
+// Joins the parts of a row.  Wave w merges the lists of the parts w, w + 4, ..
+// (two on their way at a time), then the first wave the four that remain.
+template <typename T, bool TOP>
+__global__ void __launch_bounds__(kThreads) score_join_kernel(ScoreParams p) {
+  __shared__ Entry lists[kWaves][64];
+  const int lane = threadIdx.x % 64;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
+  const int64_t row = blockIdx.x;
+  Entry best{kNone, -1};
+  if (TOP) {
+    const auto load = [&](int part) {
+      Entry e{kNone, -1};
+      if (part < p.splits && lane < p.top) {
+        const int64_t at = (row * p.splits + part) * p.top + lane;
+        e = {p.cand_val[at], p.cand_id[at]};
+      }
+      return e;
+    };
+    best = load(wave);
+    Entry next = load(wave + kWaves);
+    for (int part = wave + kWaves; part < p.splits; part += kWaves) {
+      const Entry now = next;
+      next = load(part + kWaves);
+      merge64(best, now);
+    }
+    lists[wave][lane] = best;
+    __syncthreads();
+  }
+  if (wave != 0) return;
   Sums a{kNone, 0.f, 0.f};
   if (lane < p.splits) {
-    const ScorePart b = p.part[piece];
+    const ScorePart b = p.part[row * p.splits + lane];
     a = {b.m, b.s, b.t};
   }
 #pragma unroll
@@ -330,41 +377,10 @@ __global__ void __launch_bounds__(64) score_join_kernel(ScoreParams p) {
     const Sums b{__shfl_xor(a.m, mask), __shfl_xor(a.s, mask), __shfl_xor(a.t, mask)};
     a = join(a, b);
   }
-  float val = kNone;
-  int id = -1, head = 0;
-  float hv = kNone;
-  int hi = -1;
-  if (p.top > 0 && lane < p.splits) {
-    hv = p.cand_val[piece * p.top];
-    hi = p.cand_id[piece * p.top];
-  }
-  for (int k = 0; k < p.top; ++k) {
-    float bv = hv;
-    int bi = hi;
+  if (TOP)
 #pragma unroll
-    for (int mask = 1; mask < 64; mask <<= 1) {
-      const float ov = __shfl_xor(bv, mask);
-      const int oi = __shfl_xor(bi, mask);
-      if (better(ov, oi, bv, bi)) {
-        bv = ov;
-        bi = oi;
-      }
-    }
-    if (lane == k) {
-      val = bv;
-      id = bi;
-    }
-    if (bi >= 0 && hi == bi) {  // ids are unique in a row: this lane's head was taken
-      ++head;
-      hv = kNone;
-      hi = -1;
-      if (head < p.top) {
-        hv = p.cand_val[piece * p.top + head];
-        hi = p.cand_id[piece * p.top + head];
-      }
-    }
-  }
-  write_row<T>(p, row, a, val, id);
+    for (int w = 1; w < kWaves; ++w) merge64(best, lists[w][lane]);
+  write_row<T>(p, row, a, best.val, best.id);
 }
 
 template <typename T>
@@ -374,9 +390,12 @@ hipError_t launch_typed(const ScoreParams& p, hipStream_t s) {
     score_kernel<T, true><<<dim3(blocks), kThreads, 0, s>>>(p);
   else
     score_kernel<T, false><<<dim3(blocks), kThreads, 0, s>>>(p);
-  hipError_t e = hipGetLastError();
+  const hipError_t e = hipGetLastError();
   if (e != hipSuccess || p.splits == 1) return e;
-  score_join_kernel<T><<<dim3(static_cast<uint32_t>(p.T)), 64, 0, s>>>(p);
+  if (p.top > 0)
+    score_join_kernel<T, true><<<dim3(static_cast<uint32_t>(p.T)), kThreads, 0, s>>>(p);
+  else
+    score_join_kernel<T, false><<<dim3(static_cast<uint32_t>(p.T)), 64, 0, s>>>(p);
   return hipGetLastError();
 }
 
