@@ -7,6 +7,7 @@ not a gfx950, the calls raise.
 """
 from __future__ import annotations
 
+import contextlib
 import ctypes
 import os
 
@@ -607,13 +608,12 @@ def gather(store, idx, out_dtype=None, stream=None):
 # library cannot see (types, shapes, strides and devices of the tensors).
 def _same(name, t, dtype, shape, device, contiguous=True):
     """t is a tensor of that type, shape and device (and contiguous), or a ValueError."""
-    if t.dtype != dtype or tuple(t.shape) != tuple(shape):
-        raise ValueError("%s must be %s %s, not %s %s" % (name, dtype, list(shape), t.dtype,
-                                                          list(t.shape)))
-    if t.device != device:
-        raise ValueError("%s is on %s, not on %s" % (name, t.device, device))
-    if contiguous and not t.is_contiguous():
-        raise ValueError("%s must be contiguous" % name)
+    if t.dtype is dtype and t.shape == shape and t.get_device() == device and \
+            (not contiguous or t.is_contiguous()):
+        return
+    raise ValueError("%s must be %s%s %s on cuda:%d, not %s %s with strides %s on %s"
+                     % (name, "contiguous " if contiguous else "", dtype, list(shape), device,
+                        t.dtype, list(t.shape), list(t.stride()), t.device))
 
 
 def _code(name, dtype, allowed):
@@ -627,67 +627,65 @@ _STATE = (torch.float32, torch.float16)
 
 
 def _device_of(t):
-    """t's device, which must be the current one: the library launches there."""
+    """Number of t's device, which must be the current one: the library launches there."""
     if not t.is_cuda:
         raise ValueError("tensors must be on the GPU, not on %s" % t.device)
-    if t.device.index != torch.cuda.current_device():
-        raise ValueError("tensors are on %s but the current device is cuda:%d"
-                         % (t.device, torch.cuda.current_device()))
-    return t.device
+    device = t.get_device()
+    if device != torch._C._cuda_getDevice():
+        raise ValueError("tensors are on cuda:%d but the current device is cuda:%d"
+                         % (device, torch._C._cuda_getDevice()))
+    return device
 
 
 def _token_stride(name, t, lead):
-    """Elements between tokens of t, whose first `lead` axes are the tokens' (a
-    [B, L] batch, or one packed axis) and whose others are one token, which has
-    to be dense: a slice of a wider tensor's last axis is."""
-    inner = 1
-    for n, st in zip(reversed(t.shape[lead:]), reversed(t.stride()[lead:])):
-        if n != 1 and st != inner:
-            raise ValueError("%s: the elements of one token must be contiguous" % name)
-        inner *= n
-    if t.numel() == 0:
+    """Elements between tokens of t (0: it is dense), whose first `lead` axes are
+    the tokens' (a [B, L] batch, or one packed axis) and whose others are one
+    token, which has to be dense: a slice of a wider tensor's last axis is."""
+    if t.is_contiguous():
         return 0
-    stride = t.stride(lead - 1) if t.shape[lead - 1] > 1 else 0
-    if lead == 2 and t.shape[0] > 1:
-        outer = t.stride(0)
-        if stride == 0:
-            stride = outer // t.shape[1]
-        if outer != stride * t.shape[1]:
+    shape, strides, inner = t.shape, t.stride(), 1
+    for i in range(len(shape) - 1, lead - 1, -1):
+        if shape[i] != 1 and strides[i] != inner:
+            raise ValueError("%s: the elements of one token must be contiguous" % name)
+        inner *= shape[i]
+    stride = strides[lead - 1]
+    if lead == 2 and shape[0] > 1:
+        if shape[1] == 1:
+            stride = strides[0]
+        elif strides[0] != stride * shape[1]:
             raise ValueError("%s: the rows of a batch must follow one another" % name)
-    return 0 if stride == inner else stride
+    elif shape[lead - 1] == 1:
+        return 0
+    if stride < inner:
+        raise ValueError("%s: tokens must not overlap" % name)
+    return stride
 
 
-class _Allocate:
-    """Outputs and workspace come from the stream that the kernels run on."""
-
-    def __init__(self, stream):
-        if isinstance(stream, int):
-            stream = torch.cuda.ExternalStream(stream)
-        self.scope = None if stream is None else torch.cuda.stream(stream)
-
-    def __enter__(self):
-        if self.scope is not None:
-            self.scope.__enter__()
-
-    def __exit__(self, *exc):
-        if self.scope is not None:
-            self.scope.__exit__(*exc)
+def _own_stream(stream):
+    """Context in which torch allocates from the stream that the kernels run on."""
+    if stream is None:
+        return contextlib.nullcontext()
+    return torch.cuda.stream(torch.cuda.ExternalStream(stream) if isinstance(stream, int)
+                             else stream)
 
 
 def _delta_args(q, k, v, g, beta, lead, out_dtype, state_dtype):
     dev = _device_of(k)
     if k.dim() != lead + 2 or v.dim() != lead + 2:
         raise ValueError("k and v must have %d axes" % (lead + 2))
-    code = _code("k", k.dtype, _IO)
+    dtype = k.dtype
+    code = _code("k", dtype, _IO)
     tokens, (Hk, K), (Hv, V) = k.shape[:lead], k.shape[lead:], v.shape[lead:]
     if q is not None:
-        _same("q", q, k.dtype, k.shape, dev, contiguous=False)
-    _same("v", v, k.dtype, tuple(tokens) + (Hv, V), dev, contiguous=False)
-    for name, t in (("g", g), ("beta", beta)):
-        if t is not None:
-            _same(name, t, torch.float32, tuple(tokens) + (Hv,), dev)
-    strides = [0 if t is None else _token_stride(n, t, lead)
-               for n, t in (("q", q), ("k", k), ("v", v))]
+        _same("q", q, dtype, k.shape, dev, False)
+    _same("v", v, dtype, tokens + (Hv, V), dev, False)
+    gates = tokens + (Hv,)
+    if g is not None:
+        _same("g", g, torch.float32, gates, dev)
+    if beta is not None:
+        _same("beta", beta, torch.float32, gates, dev)
+    strides = (0 if q is None else _token_stride("q", q, lead), _token_stride("k", k, lead),
+               _token_stride("v", v, lead))
     return dev, (Hk, Hv, K, V), (code, _code("out_dtype", out_dtype, _IO),
                                  _code("state_dtype", state_dtype, _STATE)), strides
 
@@ -726,7 +724,7 @@ def delta(q, k, v, g=None, beta=None, h0=None, *, starts=None, h0_idx=None, qk_n
     if hT is not None:
         _same("hT", hT, state_dtype, (B, Hv, K, V), dev)
     desc = delta_desc(B, L, Hk, Hv, K, V, *codes, *strides, 0, 0, qk_norm, eps, scale)
-    with _Allocate(stream):
+    with _own_stream(stream):
         o = torch.empty(tuple(v.shape), dtype=out_dtype, device=dev) if want_o else None
         if want_hT and hT is None:
             hT = torch.empty((B, Hv, K, V), dtype=state_dtype, device=dev)
@@ -748,7 +746,7 @@ def delta_step(q, k, v, g, beta, states, slots, *, qk_norm=False, eps=1e-6, scal
     _same("states", states, states.dtype, (states.shape[0], Hv, K, V), dev)
     _same("slots", slots, torch.int32, (n,), dev)
     desc = delta_desc(n, 1, Hk, Hv, K, V, *codes, *strides, 0, 0, qk_norm, eps, scale)
-    with _Allocate(stream):
+    with _own_stream(stream):
         o = torch.empty((n, Hv, V), dtype=out_dtype, device=dev) if want_o else None
     delta_step_raw(desc, q, k, v, g, beta, states, states.shape[0], slots, o, stream)
     return o
@@ -792,7 +790,7 @@ def conv(x, w, bias=None, tail0=None, *, starts=None, tail_idx=None, silu=True, 
     if tailT is not None:
         _same("tailT", tailT, x.dtype, (B, W - 1, D), dev)
     desc = conv_desc(B, L, D, W, *codes, stride, silu)
-    with _Allocate(stream):
+    with _own_stream(stream):
         y = torch.empty(tuple(x.shape), dtype=out_dtype, device=dev) if want_y else None
         if want_tail and tailT is None:
             tailT = torch.empty((B, max(W - 1, 0), D), dtype=x.dtype, device=dev)
@@ -811,7 +809,7 @@ def conv_step(x, w, bias, tails, slots, *, silu=True, out_dtype=None, stream=Non
     _same("tails", tails, x.dtype, (tails.shape[0], W - 1, D), dev)
     _same("slots", slots, torch.int32, (n,), dev)
     desc = conv_desc(n, 1, D, W, *codes, stride, silu)
-    with _Allocate(stream):
+    with _own_stream(stream):
         y = torch.empty((n, D), dtype=out_dtype, device=dev)
     conv_step_raw(desc, x, w, bias, tails, tails.shape[0], slots, y, stream)
     return y
@@ -833,7 +831,7 @@ def score_tokens(logits, token=None, top=0, *, want_entropy=True, stream=None):
     if token is not None:
         _same("token", token, torch.int32, (T,), dev)
     nbytes = score_workspace_bytes(T, V, top)
-    with _Allocate(stream):
+    with _own_stream(stream):
         logprob = torch.empty(T, dtype=torch.float32, device=dev) if token is not None else None
         entropy = torch.empty(T, dtype=torch.float32, device=dev) if want_entropy else None
         top_id = torch.empty((T, top), dtype=torch.int32, device=dev) if top else None

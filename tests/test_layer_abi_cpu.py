@@ -166,6 +166,13 @@ def test_token_strides():
     assert P._token_stride("t", base, 2) == 0
     assert P._token_stride("t", base[0, :, 8:72].unflatten(1, (2, 32)), 1) == 100
     assert P._token_stride("t", base[:, ::2], 2) == 200
+    assert P._token_stride("t", base[:, :1, :64], 2) == 400   # one token a row
+    assert P._token_stride("t", base[:1, :, :64], 2) == 100
+    assert P._token_stride("t", base[0, :1, :64], 1) == 0
+    for t, lead in ((torch.zeros(1, 64).expand(5, 64), 1), (torch.zeros(1, 4, 64).expand(3, 4, 64), 2),
+                    (torch.zeros(5, 1, 64).expand(5, 2, 64), 1)):
+        with pytest.raises(ValueError):
+            P._token_stride("t", t, lead)           # the same elements for several tokens
     with pytest.raises(ValueError):
         P._token_stride("t", base.transpose(1, 2), 2)
     with pytest.raises(ValueError):
