@@ -1,7 +1,12 @@
 // The short causal depthwise convolution: every lane owns eight channels and
 // slides the last W - 1 inputs of them over a run of tokens in registers, so
 // each input is read once (and the W - 1 before a run once more).  Memory
-// bounds it: W multiply-adds and one exponential an element.
+// bounds it: W multiply-adds and one exponential an element.  The four waves of
+// a workgroup take neighbouring channels of the same tokens, 4 KB of a bf16 row
+// (48 packed documents of 4,096 channels: 305 us with four runs of tokens side
+// by side, 270 us so with streamed stores), and four of them share a SIMD: with
+// four tokens on their way in each, instead of eight, nothing spills at 128
+// registers (262 us, 4.2 TB/s).
 #include "layer_ops.h"
 
 namespace precog {
@@ -9,9 +14,10 @@ namespace {
 
 constexpr int kLaneCh = 8;                // channels of a lane: 16 bytes of bf16
 constexpr int kWaveCh = 64 * kLaneCh;
-constexpr int kConvWaves = 4;             // runs of a workgroup
-constexpr int kRun = 32;                  // tokens of a run
-constexpr int kAhead = 8;                 // tokens loaded at a time
+constexpr int kConvWaves = 4;             // waves of a workgroup, beside one another in the channels
+constexpr int kAhead = 4;                 // tokens loaded at a time
+constexpr int kRunMost = 32, kRunLeast = 8;  // tokens of a run
+constexpr int64_t kL2Bytes = 32LL << 20;  // of the 8 XCDs
 
 // Input j (0 = oldest) of the W - 1 before the first token of sequence b.
 template <typename TIn>
@@ -46,7 +52,27 @@ __device__ __forceinline__ void load_taps(const ConvParams& p, int64_t d, float 
 }
 
 // One token: the sum over the window and the new input, then the window moves on.
-template <typename TOut, int W>
+// Stores eight results; streamed past the cache if the call's do not fit there.
+template <bool STREAM, typename TOut>
+__device__ __forceinline__ void store_out(TOut* y, const float (&f)[kLaneCh]) {
+  if constexpr (!STREAM) {
+    store_pack<kLaneCh>(y, f);
+    return;
+  }
+  typedef uint32_t uint4v __attribute__((ext_vector_type(4)));
+  Pack<TOut, kLaneCh> r;
+#pragma unroll
+  for (int i = 0; i < kLaneCh; ++i) r.v[i] = narrow<TOut>(f[i]);
+  struct Words {
+    uint4v w[sizeof(r) / 16];
+  };
+  const Words words = __builtin_bit_cast(Words, r);
+#pragma unroll
+  for (int i = 0; i < static_cast<int>(sizeof(r) / 16); ++i)
+    __builtin_nontemporal_store(words.w[i], reinterpret_cast<uint4v*>(y) + i);
+}
+
+template <bool STREAM, typename TOut, int W>
 __device__ __forceinline__ void conv_token(const float (&w)[W][kLaneCh], const float (&bias)[kLaneCh],
                                            float (&win)[W - 1][kLaneCh], const float (&x)[kLaneCh],
                                            int silu, TOut* y) {
@@ -63,7 +89,7 @@ __device__ __forceinline__ void conv_token(const float (&w)[W][kLaneCh], const f
     for (int j = 0; j + 2 < W; ++j) win[j][c] = win[j + 1][c];
     win[W - 2][c] = x[c];
   }
-  store_pack<kLaneCh>(y, out);
+  store_out<STREAM>(y, out);
 }
 
 // The tail behind sequence b: the last W - 1 of its tail and its tokens.
@@ -90,21 +116,19 @@ __device__ __forceinline__ void capture_tail(const ConvParams& p, int64_t b, int
     if (j < p.W - 1) store_pack<kLaneCh>(static_cast<TIn*>(p.tailT) + (b * (p.W - 1) + j) * p.D + d, keep[j]);
 }
 
-// Workgroups [0, run_blocks): kConvWaves runs of kRun tokens.  Those behind:
-// kConvWaves sequences' tails.
-template <typename TIn, typename TOut, int W>
-__global__ void __launch_bounds__(64 * kConvWaves) conv_kernel(ConvParams p, int64_t run_blocks) {
+// Workgroups [0, run_blocks): a run of `run` tokens.  Those behind: a sequence's
+// tail.
+template <typename TIn, typename TOut, int W, bool STREAM>
+__global__ void __launch_bounds__(64 * kConvWaves) __attribute__((amdgpu_waves_per_eu(4))) conv_kernel(ConvParams p, int64_t run_blocks, int run) {
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
-  const int64_t d = static_cast<int64_t>(blockIdx.y) * kWaveCh + (threadIdx.x % 64) * kLaneCh;
+  const int64_t d = (static_cast<int64_t>(blockIdx.y) * (blockDim.x / 64) + wave) * kWaveCh + (threadIdx.x % 64) * kLaneCh;
   if (d >= p.D) return;
   if (static_cast<int64_t>(blockIdx.x) >= run_blocks) {
-    const int64_t b = (blockIdx.x - run_blocks) * kConvWaves + wave;
-    if (b < p.B) capture_tail<TIn>(p, b, d);
+    capture_tail<TIn>(p, blockIdx.x - run_blocks, d);
     return;
   }
-  const int64_t first = (static_cast<int64_t>(blockIdx.x) * kConvWaves + wave) * kRun;
-  const int64_t last = first + kRun < p.T ? first + kRun : p.T;
-  if (first >= last) return;
+  const int64_t first = static_cast<int64_t>(blockIdx.x) * run;
+  const int64_t last = first + run < p.T ? first + run : p.T;
 
   // the last sequence that begins at or before the run's first token
   int64_t b = 0;
@@ -152,7 +176,7 @@ __global__ void __launch_bounds__(64 * kConvWaves) conv_kernel(ConvParams p, int
           float v[kLaneCh];
 #pragma unroll
           for (int c = 0; c < kLaneCh; ++c) v[c] = widen(in[i].v[c]);
-          conv_token<TOut, W>(w, bias, win, v, p.silu, y + (t + i) * p.D);
+          conv_token<STREAM, TOut, W>(w, bias, win, v, p.silu, y + (t + i) * p.D);
         }
       }
     }
@@ -190,7 +214,7 @@ __global__ void __launch_bounds__(64) conv_step_kernel(ConvParams p) {
 #pragma unroll
     for (int c = 0; c < kLaneCh; ++c) v[c] = widen(in.v[c]);
     if (p.y != nullptr) {
-      conv_token<TOut, W>(w, bias, win, v, p.silu, static_cast<TOut*>(p.y) + row * p.D + d);
+      conv_token<false, TOut, W>(w, bias, win, v, p.silu, static_cast<TOut*>(p.y) + row * p.D + d);
     } else {
 #pragma unroll
       for (int c = 0; c < kLaneCh; ++c) {
@@ -225,17 +249,27 @@ hipError_t launch_conv(const ConvParams& p, int in_dtype, int out_dtype, int cus
     using TIn = decltype(in);
     using TOut = decltype(out);
     constexpr int W = decltype(width)::value;
-    const uint32_t cols = static_cast<uint32_t>((p.D + kWaveCh - 1) / kWaveCh);
-    const int64_t per = static_cast<int64_t>(kConvWaves) * kRun;
-    const int64_t runs = p.y != nullptr ? (p.T + per - 1) / per : 0;
-    const int64_t tails = p.tailT != nullptr ? (p.B + kConvWaves - 1) / kConvWaves : 0;
+    const int64_t wave_cols = (p.D + kWaveCh - 1) / kWaveCh;
+    const int waves = static_cast<int>(wave_cols < kConvWaves ? wave_cols : kConvWaves);
+    const uint32_t cols = static_cast<uint32_t>((wave_cols + waves - 1) / waves);
+    // runs of 32 tokens where eight waves a CU remain, else down to 8 (3 x 1,001
+    // tokens of 1,000 fp32 channels: 23 us a call with 32, 15 us with 8)
+    int run = kRunMost;
+    while (run > kRunLeast && (p.T + run - 1) / run * wave_cols < 8LL * cus) run /= 2;
+    const int64_t runs = p.y != nullptr ? (p.T + run - 1) / run : 0;
+    const int64_t tails = p.tailT != nullptr ? p.B : 0;
+    const bool streamed = p.T * p.D * static_cast<int64_t>(sizeof(TOut)) > kL2Bytes;
     // in place, the runs read tails that the capture replaces: then it goes
     // behind them, in a launch of its own
     const bool apart = p.tail0 != nullptr && p.tail0 == p.tailT && runs > 0;
-    conv_kernel<TIn, TOut, W><<<dim3(static_cast<uint32_t>(runs + (apart ? 0 : tails)), cols), 64 * kConvWaves, 0, s>>>(p, runs);
+    const dim3 grid(static_cast<uint32_t>(runs + (apart ? 0 : tails)), cols);
+    if (streamed)
+      conv_kernel<TIn, TOut, W, true><<<grid, 64 * waves, 0, s>>>(p, runs, run);
+    else
+      conv_kernel<TIn, TOut, W, false><<<grid, 64 * waves, 0, s>>>(p, runs, run);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess || !apart || tails == 0) return e;
-    conv_kernel<TIn, TOut, W><<<dim3(static_cast<uint32_t>(tails), cols), 64 * kConvWaves, 0, s>>>(p, 0);
+    conv_kernel<TIn, TOut, W, false><<<dim3(static_cast<uint32_t>(tails), cols), 64 * waves, 0, s>>>(p, 0, run);
     return hipGetLastError();
   });
 }
