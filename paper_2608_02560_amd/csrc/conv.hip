@@ -193,7 +193,7 @@ __global__ void __launch_bounds__(64) conv_step_kernel(ConvParams p) {
   const int64_t d = static_cast<int64_t>(blockIdx.y) * kWaveCh + tid * kLaneCh;
   const int64_t slot = p.idx[b];
   if (slot < 0 || slot >= p.tail_rows) return;
-  if (!leads_slot(p.idx, p.B, b, static_cast<int32_t>(slot), tid, 64)) return;
+  if (!leads_slot(p.idx, b, static_cast<int32_t>(slot), tid, 64)) return;
   const bool on = d < p.D;
   TIn* tail = static_cast<TIn*>(p.tailT) + slot * (W - 1) * p.D + d;
   float w[W][kLaneCh], bias[kLaneCh], win[W - 1][kLaneCh];

@@ -1,10 +1,12 @@
-// The gated delta rule token by token: one workgroup keeps CT columns of one
-// head's [K, V] state in registers and applies its tokens in order.
+// One token of each of many sessions through the gated delta rule: a workgroup
+// keeps CT columns of one head's [K, V] state in registers for it.
 //
 //   u = beta (v - a S^T k),  S <- a S + k u^T,  o = scale (a S^T q + (k.q) u)
 //
 // with S the state before the token: S^T k and S^T q come out of one pass over
-// the state and one reduction, and the state is read and written once.
+// the state and one reduction, and the state is read and written once, which is
+// what bounds it: 96 sessions of 16 heads of 128 x 128 fp32 states, 201 MB, take
+// 43 us, 4.7 TB/s, the rate of a large copy (35 us where they are in the cache).
 #include "layer_ops.h"
 
 namespace precog {
@@ -13,8 +15,37 @@ namespace {
 constexpr int kThreads = 256;
 constexpr int kWaves = kThreads / 64;
 
-template <typename TIn, typename TOut, typename TSt, int CT, bool STEP>
-__global__ void __launch_bounds__(kThreads) delta_rows_kernel(DeltaParams p) {
+typedef uint32_t uint2v __attribute__((ext_vector_type(2)));
+typedef uint32_t uint4v __attribute__((ext_vector_type(4)));
+
+template <typename T>
+__device__ __forceinline__ void load_four(__amdgpu_buffer_rsrc_t r, uint32_t off, float (&f)[4]) {
+  if constexpr (sizeof(T) == 4) {
+    const uint4v v = __builtin_bit_cast(uint4v, __builtin_amdgcn_raw_buffer_load_b128(r, off, 0, 0));
+#pragma unroll
+    for (int c = 0; c < 4; ++c) f[c] = __uint_as_float(v[c]);
+  } else {
+    const uint2v v = __builtin_bit_cast(uint2v, __builtin_amdgcn_raw_buffer_load_b64(r, off, 0, 0));
+#pragma unroll
+    for (int c = 0; c < 4; ++c) f[c] = widen(T{static_cast<uint16_t>(v[c / 2] >> 16 * (c % 2))});
+  }
+}
+template <typename T>
+__device__ __forceinline__ void store_four(__amdgpu_buffer_rsrc_t r, uint32_t off, const float (&f)[4]) {
+  if constexpr (sizeof(T) == 4) {
+    __builtin_amdgcn_raw_buffer_store_b128(
+        uint4v{__float_as_uint(f[0]), __float_as_uint(f[1]), __float_as_uint(f[2]), __float_as_uint(f[3])}, r, off, 0, 0);
+  } else {
+    uint2v v;
+#pragma unroll
+    for (int c = 0; c < 2; ++c)
+      v[c] = narrow<T>(f[2 * c]).bits | static_cast<uint32_t>(narrow<T>(f[2 * c + 1]).bits) << 16;
+    __builtin_amdgcn_raw_buffer_store_b64(v, r, off, 0, 0);
+  }
+}
+
+template <typename TIn, typename TOut, typename TSt, int CT>
+__global__ void __launch_bounds__(kThreads) delta_step_kernel(DeltaParams p) {
   constexpr int kLanes = CT / 4;            // threads across the columns, four each
   constexpr int kGroups = kThreads / kLanes;  // row groups
   constexpr int kRows = kDeltaMaxK / kGroups;
@@ -34,37 +65,22 @@ __global__ void __launch_bounds__(kThreads) delta_rows_kernel(DeltaParams p) {
   const int col = cb * CT + 4 * cl;
   const bool on = col < p.V;
 
-  int64_t row = b;
-  bool known = true;
-  if (p.idx != nullptr) {
-    row = p.idx[b];
-    known = row >= 0 && row < p.state_rows;
-  }
-  if (STEP) {
-    if (!known) return;
-    if (!leads_slot(p.idx, p.B, b, static_cast<int32_t>(row), tid, kThreads)) return;
-  }
-  const int64_t at = (static_cast<int64_t>(h) * p.K) * p.V + col;
+  const int32_t slot = p.idx[b];
+  if (slot < 0 || slot >= p.state_rows) return;
+  if (!leads_slot(p.idx, b, slot, tid, kThreads)) return;
+  // the head's state as a buffer: rows from K on lie past its end, read as zeros
+  // and are not written
+  constexpr uint32_t kSize = sizeof(TSt);
+  const __amdgpu_buffer_rsrc_t state =
+      make_rsrc(static_cast<TSt*>(p.hT) + slot * p.h0_stride + static_cast<int64_t>(h) * p.K * p.V,
+                static_cast<uint32_t>(p.K * p.V) * kSize);
+  const uint32_t at = on ? static_cast<uint32_t>(rg * p.V + col) * kSize : kDropOffset;
+  const uint32_t step = static_cast<uint32_t>(kGroups * p.V) * kSize;
   float S[kRows][4];
-  const TSt* h0 = static_cast<const TSt*>(p.h0);
 #pragma unroll
-  for (int i = 0; i < kRows; ++i) {
-    const int r = rg + kGroups * i;
-    const bool in = on && r < p.K;
-    if (in && h0 != nullptr && known) {
-      const Pack<TSt, 4> s = load_pack<4>(h0 + row * p.h0_stride + at + static_cast<int64_t>(r) * p.V);
-#pragma unroll
-      for (int c = 0; c < 4; ++c) S[i][c] = widen(s.v[c]);
-    } else {
-#pragma unroll
-      for (int c = 0; c < 4; ++c) S[i][c] = known ? 0.f : __builtin_nanf("");
-    }
-  }
+  for (int i = 0; i < kRows; ++i) load_four<TSt>(state, at + i * step, S[i]);
 
-  const Span span = STEP ? Span{b, b + 1} : sequence(p.starts, b, p.L, p.T);
-  int64_t t = span.begin;
-  while (STEP ? t >= 0 : t < span.end) {
-    __syncthreads();
+  for (int64_t t = b;;) {  // this row, then the others of the slot
     {  // waves 0 and 1 prepare k, waves 2 and 3 q
       const int which = tid / 128, i = tid % 128;
       float x = 0.f;
@@ -139,56 +155,43 @@ __global__ void __launch_bounds__(kThreads) delta_rows_kernel(DeltaParams p) {
         for (int c = 0; c < 4; ++c) S[i][c] = a * S[i][c] + kr * u[c];
       }
     }
-    if (STEP) {
-      t = next_of_slot(p.idx, p.B, t, static_cast<int32_t>(row), tid, kThreads, &next_row);
-      if (t >= 0)  // as a call of its own would store and load the state
+    t = next_of_slot(p.idx, p.B, t, slot, tid, kThreads, &next_row);
+    if (t < 0) break;
+    // as a call of its own would store and load the state
 #pragma unroll
-        for (int i = 0; i < kRows; ++i)
+    for (int i = 0; i < kRows; ++i)
 #pragma unroll
-          for (int c = 0; c < 4; ++c) S[i][c] = widen(narrow<TSt>(S[i][c]));
-    } else {
-      ++t;
-    }
+      for (int c = 0; c < 4; ++c) S[i][c] = widen(narrow<TSt>(S[i][c]));
   }
-  if (p.hT != nullptr && on) {
-    TSt* hT = static_cast<TSt*>(p.hT) + (STEP ? row : b) * p.hT_stride + at;
 #pragma unroll
-    for (int i = 0; i < kRows; ++i) {
-      const int r = rg + kGroups * i;
-      if (r < p.K) store_pack<4>(hT + static_cast<int64_t>(r) * p.V, S[i]);
-    }
-  }
+  for (int i = 0; i < kRows; ++i) store_four<TSt>(state, at + i * step, S[i]);
 }
 
-template <typename TIn, typename TOut, typename TSt, bool STEP>
-hipError_t launch_rows(const DeltaParams& p, int cus, hipStream_t s) {
-  const auto blocks = [&](int ct) { return p.B * p.Hv * ((p.V + ct - 1) / ct); };
-  if (blocks(128) >= 4LL * cus)
-    delta_rows_kernel<TIn, TOut, TSt, 128, STEP><<<dim3(static_cast<uint32_t>(blocks(128))), kThreads, 0, s>>>(p);
+template <typename TIn, typename TOut, typename TSt>
+hipError_t launch_typed(const DeltaParams& p, int cus, hipStream_t s) {
+  // all 128 columns a workgroup where that leaves four of them a CU, else 32:
+  // a single session's eight heads are 16 workgroups rather than 8
+  const auto blocks = [&](int ct) { return static_cast<uint32_t>(p.B * p.Hv * ((p.V + ct - 1) / ct)); };
+  if (blocks(128) >= 4u * cus)
+    delta_step_kernel<TIn, TOut, TSt, 128><<<dim3(blocks(128)), kThreads, 0, s>>>(p);
   else
-    delta_rows_kernel<TIn, TOut, TSt, 32, STEP><<<dim3(static_cast<uint32_t>(blocks(32))), kThreads, 0, s>>>(p);
+    delta_step_kernel<TIn, TOut, TSt, 32><<<dim3(blocks(32)), kThreads, 0, s>>>(p);
   return hipGetLastError();
-}
-
-template <bool STEP>
-hipError_t by_types(const DeltaParams& p, int in_dtype, int out_dtype, int state_dtype, int cus,
-                    hipStream_t s) {
-  const auto st = [&](auto in, auto out) {
-    using TIn = decltype(in);
-    using TOut = decltype(out);
-    return state_dtype == PRECOG_F32 ? launch_rows<TIn, TOut, float, STEP>(p, cus, s)
-                                     : launch_rows<TIn, TOut, f16_t, STEP>(p, cus, s);
-  };
-  if (in_dtype == PRECOG_F32)
-    return out_dtype == PRECOG_F32 ? st(float{}, float{}) : st(float{}, bf16_t{});
-  return out_dtype == PRECOG_F32 ? st(bf16_t{}, float{}) : st(bf16_t{}, bf16_t{});
 }
 
 }  // namespace
 
 hipError_t launch_delta_step(const DeltaParams& p, int in_dtype, int out_dtype, int state_dtype,
                              int cus, hipStream_t s) {
-  return by_types<true>(p, in_dtype, out_dtype, state_dtype, cus, s);
+  const auto typed = [&](auto in, auto out) {
+    using TIn = decltype(in);
+    using TOut = decltype(out);
+    return state_dtype == PRECOG_F32 ? launch_typed<TIn, TOut, float>(p, cus, s)
+                                     : launch_typed<TIn, TOut, f16_t>(p, cus, s);
+  };
+  if (in_dtype == PRECOG_F32)
+    return out_dtype == PRECOG_F32 ? typed(float{}, float{}) : typed(float{}, bf16_t{});
+  return out_dtype == PRECOG_F32 ? typed(bf16_t{}, float{}) : typed(bf16_t{}, bf16_t{});
 }
 
 }  // namespace precog

@@ -202,6 +202,7 @@ precog_status precog_delta_step(const precog_delta_desc* desc, const void* q, co
   precog_status st = validate_delta(desc, true);
   if (st != PRECOG_OK) return st;
   if (state_rows < 0) return PRECOG_ERR_SHAPE;
+  if (desc->batch * desc->v_heads > kMaxTokens / 8) return PRECOG_ERR_SHAPE;  // workgroups, 8 a head at most
   if (desc->batch == 0) return PRECOG_OK;
   if (!k || !v || !slots || (o && !q) || (state_rows > 0 && !states)) return PRECOG_ERR_NULL;
   for (const void* p : {q, k, v, static_cast<const void*>(states), static_cast<const void*>(o)})

@@ -63,8 +63,7 @@ __device__ __forceinline__ Span sequence(const int32_t* starts, int64_t b, int64
 // The row of a step (precog_delta_step, precog_conv_step): whether a call's
 // row b leads its slot's rows, and the next row of the same slot after `row`.
 // Every thread of the workgroup calls these; `shared` is one int of LDS.
-__device__ __forceinline__ bool leads_slot(const int32_t* slots, int64_t n, int64_t b, int32_t slot,
-                                           int tid, int threads) {
+__device__ __forceinline__ bool leads_slot(const int32_t* slots, int64_t b, int32_t slot, int tid, int threads) {
   int earlier = 0;
   for (int64_t j = tid; j < b; j += threads) earlier |= slots[j] == slot;
   return __syncthreads_or(earlier) == 0;

@@ -828,6 +828,8 @@ def score_tokens(logits, token=None, top=0, *, want_entropy=True, stream=None):
     if V > 1 and logits.stride(1) != 1:
         raise ValueError("logits: the elements of a row must be contiguous")
     stride = logits.stride(0) if T > 1 else V
+    if stride < V:
+        raise ValueError("logits: rows must not overlap")
     if token is not None:
         _same("token", token, torch.int32, (T,), dev)
     nbytes = score_workspace_bytes(T, V, top)

@@ -101,6 +101,7 @@ def test_step_arguments():
         assert _step(good, **{name: FAKE + 2}) == EALIGN
     assert _step(good, rows=-1) == ESHAPE
     assert _step(P.delta_desc(65536, 1, 2, 4, 64, 64)) == ESHAPE
+    assert _step(P.delta_desc(65535, 1, 1, 8192, 8, 8)) == ESHAPE
 
 
 @pytest.mark.parametrize("bad,code", [
