@@ -547,6 +547,11 @@ typedef struct {
     float scale;      /* factor of o; 0 = 1 / sqrt(k_dim) */
 } precog_delta_desc;
 
+/* Bytes of device workspace precog_delta_encode needs for this descriptor,
+ * `packed` nonzero for a call with `starts`: 0 unless long sequences have few
+ * heads, which are then computed in segments.  0 for a descriptor it refuses. */
+size_t precog_delta_workspace_bytes(const precog_delta_desc *desc, int packed);
+
 /* The gated delta rule: the second kind of layer whose state can be stored
  * and injected as in Sec. 4.2.  Each value head keeps a [K, V] matrix that
  * forgets by a_t = exp(g_t) and has its value for key k_t replaced by v_t to
@@ -579,13 +584,16 @@ typedef struct {
  *              h0_idx (in place); must not overlap h0 otherwise.
  * Arithmetic in fp32.  A NaN or an infinity in a token reaches o of its head
  * and sequence from the beginning of the token's block of 32 on.
+ *   workspace  precog_delta_workspace_bytes(desc, starts != NULL) bytes; NULL
+ *              where that is 0.
  * Alignment: pointers 16 bytes (g, beta, starts, h0_idx: 4), strides as above.
- * Deterministic; nothing but o and hT is written. */
+ * Deterministic; nothing but o, hT and the workspace is written. */
 precog_status precog_delta_encode(const precog_delta_desc *desc, const void *q,
                                   const void *k, const void *v, const float *g,
                                   const float *beta, const int32_t *starts,
                                   const void *h0, int64_t h0_rows,
                                   const int32_t *h0_idx, void *o, void *hT,
+                                  void *workspace, size_t workspace_bytes,
                                   void *stream);
 
 /* One token of each of desc->batch running sessions: the rule above for a

@@ -37,6 +37,14 @@
 // column's (T: block's) largest at 2^14, so neither half runs out of range.
 // Products of two low halves are left out (2^-22).  What only enters a bf16 o
 // (Q S, Q K^T U) takes the high halves alone: 2^-11 against the 2^-8 of o.
+//
+// Long sequences of few heads.  A head's blocks follow one another, so a call of
+// fewer heads than CUs is cut into segments of each sequence: the end state of a
+// segment is Phi S + F, where F is its end state from zeros and the columns of
+// Phi are those from unit vectors with values of zero, both computed by the same
+// blocks.  Three launches: Phi and F of every segment but the last; the states
+// between them, one after the other (join_kernel, in fp32); all segments again,
+// from those, with their outputs.  Three times the work, on all CUs.
 #include "layer_ops.h"
 #include "wave_ops.h"
 
@@ -183,6 +191,8 @@ __device__ __forceinline__ half8 high(const float4v& a, const float4v& b) {
 }
 
 __device__ __forceinline__ int exponent(float v) { return static_cast<int>(__float_as_uint(v) >> 23 & 255); }
+
+__device__ __forceinline__ int uniform(int v) { return __builtin_amdgcn_readfirstlane(v); }
 
 __device__ __forceinline__ void wait_for(const int* flag, int at_least) {
   while (__hip_atomic_load(flag, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP) < at_least)
@@ -400,7 +410,7 @@ __device__ __forceinline__ void prepare_block(const DeltaParams& p, Inputs<KP, O
     s.rk[lane] = rk;
     s.beta[lane] = in.beta;
   }
-  if (!IN32) next();
+  next();
   wave_fence();
 
   lane = fresh_lane();
@@ -553,7 +563,6 @@ __device__ __forceinline__ void prepare_block(const DeltaParams& p, Inputs<KP, O
     }
   }
   wave_fence();
-  if (IN32) next();  // 128 registers of inputs: no room beside the rest
 }
 
 // -------------------------------------------------------------------- chain
@@ -647,11 +656,23 @@ __global__ void __launch_bounds__(64 * (kChainMax + Shared<KP, IN32, OUT>::kPrep
   const int width = 16 * NV * chain_waves;
   const int vblocks = (p.V + width - 1) / width;
   // the heads that share keys follow one another, on one XCD
-  const int bid = xcd_remap(blockIdx.x, gridDim.x);
-  const int vb = bid % vblocks;
-  const int h = bid / vblocks % p.Hv;
-  const int64_t b = bid / vblocks / p.Hv;
-  const Span span = sequence(p.starts, b, p.L, p.T);
+  const int at_block = xcd_remap(blockIdx.x, gridDim.x);
+  const int column_blocks = vblocks + (p.phase == kSegmentEnds);
+  const int segments = p.phase == kSegmentEnds ? p.segments - 1 : p.segments;
+  const int vb = at_block % column_blocks;
+  const int h = uniform(at_block / column_blocks % p.Hv);
+  const int seg = uniform(at_block / column_blocks / p.Hv % segments);
+  const int64_t b = uniform(at_block / column_blocks / p.Hv / segments);
+  const bool phi = vb == vblocks;  // the columns of Phi, values of zero
+  if (phi && seg == 0) return;     // the first segment starts from the given state
+  Span span = sequence(p.starts, b, p.L, p.T);
+  if (p.segments > 1) {
+    const int first = static_cast<int>(span.begin), last = static_cast<int>(span.end);
+    const int each = ((last - first + kBlockTokens - 1) / kBlockTokens + p.segments - 1) / p.segments;  // blocks
+    const int64_t begin = first + static_cast<int64_t>(seg) * each * kBlockTokens, end = begin + each * kBlockTokens;
+    span = {begin < last ? begin : last, end < last ? end : last};
+  }
+  span = {uniform(static_cast<int>(span.begin)), uniform(static_cast<int>(span.end))};
   const int blocks = static_cast<int>((span.end - span.begin + kBlockTokens - 1) / kBlockTokens);
 
   if (threadIdx.x < Sh::kBuffers) sh.ready[threadIdx.x] = 0;
@@ -663,27 +684,45 @@ __global__ void __launch_bounds__(64 * (kChainMax + Shared<KP, IN32, OUT>::kPrep
     const int self = wave - chain_waves;
     const uint32_t k_off = Rows<KP, TIn>::lane_offset(static_cast<uint32_t>(p.k_stride * sizeof(TIn)), p.K);
     const uint32_t q_off = Rows<KP, TIn>::lane_offset(static_cast<uint32_t>(p.q_stride * sizeof(TIn)), p.K);
+    // a block's inputs are on their way while the one before is worked on, unless
+    // they take 128 registers
+    constexpr bool kAhead = !(IN32 && KP == 128);
     Inputs<KP, OUT, TIn> in;
-    if (self < blocks) in.load(p, span, self, hk, h, k_off, q_off);
+    if (kAhead && self < blocks) in.load(p, span, self, hk, h, k_off, q_off);
     for (int c = self; c < blocks; c += Sh::kPrepare) {
+      if (!kAhead) in.load(p, span, c, hk, h, k_off, q_off);
       prepare_block<KP, IN32, OUT, TIn>(p, in, sh.scratch[self], sh.buf[c % Sh::kBuffers], sh.done, chain_waves,
-                                          c - Sh::kBuffers + 1, [&] {
-                                            if (c + Sh::kPrepare < blocks)
-                                              in.load(p, span, c + Sh::kPrepare, hk, h, k_off, q_off);
-                                          });
+                                        c - Sh::kBuffers + 1, [&] {
+                                          if (kAhead && c + Sh::kPrepare < blocks)
+                                            in.load(p, span, c + Sh::kPrepare, hk, h, k_off, q_off);
+                                        });
       publish(&sh.ready[c % Sh::kBuffers], c + 1);
     }
     return;
   }
 
-  const int col = vb * width + wave * 16 * NV + m * NV;
-  if (vb * width + wave * 16 * NV >= p.V) {  // no columns: the prepare waves need not wait
+  const int wave_col = (phi ? 0 : vb * width) + wave * 16 * NV, col = wave_col + m * NV;
+  const int columns = phi ? p.K : p.V;
+  if (wave_col >= columns) {  // no columns: the prepare waves need not wait
     publish(&sh.done[wave], 0x7fffffff);
     return;
   }
   const int64_t state_at = static_cast<int64_t>(h) * p.K * p.V;
+  // state of slot `s` between the segments
+  const auto between = [&](int s) {
+    return p.between + ((b * p.segments + s) * p.Hv + h) * static_cast<int64_t>(p.K) * p.V;
+  };
   float4v S[NV][kTiles] = {};
-  {
+  if (p.phase == kSegments) {
+    load_state<KP, NV>(between((seg + p.segments - 1) % p.segments), p.V, p.K, col, S);
+  } else if (phi) {
+#pragma unroll
+    for (int n = 0; n < NV; ++n)
+#pragma unroll
+      for (int t = 0; t < kTiles; ++t)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) S[n][t][r] = 32 * (t / 2) + 8 * q + 4 * (t % 2) + r == col + n ? 1.f : 0.f;
+  } else if (seg == 0) {
     int64_t row = b;
     bool known = true;
     if (p.idx != nullptr) {
@@ -706,7 +745,7 @@ __global__ void __launch_bounds__(64 * (kChainMax + Shared<KP, IN32, OUT>::kPrep
 
   const uint32_t v_step = static_cast<uint32_t>(p.v_stride * sizeof(TIn));
   const uint32_t o_step = static_cast<uint32_t>(static_cast<int64_t>(p.Hv) * p.V * sizeof(TOut));
-  const uint32_t v_off = col < p.V ? static_cast<uint32_t>(col * sizeof(TIn)) + 4 * q * v_step : kDropOffset;
+  const uint32_t v_off = col < p.V && !phi ? static_cast<uint32_t>(col * sizeof(TIn)) + 4 * q * v_step : kDropOffset;
   const uint32_t o_off = col < p.V ? static_cast<uint32_t>(col * sizeof(TOut)) + 4 * q * o_step : kDropOffset;
   uint32_t raw[2][4][2];  // the block's values: tokens 16 t + 4 q + r
   const int tokens = static_cast<int>(span.end - span.begin);
@@ -924,11 +963,16 @@ __global__ void __launch_bounds__(64 * (kChainMax + Shared<KP, IN32, OUT>::kPrep
     publish(&sh.done[wave], c + 1);
   }
 
-  if (p.hT != nullptr) {
 #pragma unroll
-    for (int n = 0; n < NV; ++n)
+  for (int n = 0; n < NV; ++n)
 #pragma unroll
-      for (int t = 0; t < kTiles; ++t) S[n][t] *= sigma[n];
+    for (int t = 0; t < kTiles; ++t) S[n][t] *= sigma[n];
+  if (p.phase == kSegmentEnds) {
+    if (phi)
+      store_state<KP, NV>(p.phi + ((b * p.segments + seg) * p.Hv + h) * static_cast<int64_t>(p.K) * p.K, p.K, p.K, col, S);
+    else
+      store_state<KP, NV>(between(seg), p.V, p.K, col, S);
+  } else if (p.hT != nullptr && seg == p.segments - 1) {
     if (state16)
       store_state<KP, NV>(static_cast<f16_t*>(p.hT) + b * p.hT_stride + state_at, p.V, p.K, col, S);
     else
@@ -936,11 +980,106 @@ __global__ void __launch_bounds__(64 * (kChainMax + Shared<KP, IN32, OUT>::kPrep
   }
 }
 
+// The states between the segments of a sequence: slot j holds F_j (slot 0: the
+// first segment's end from the given state) and gets the end of segment j,
+// Phi_j S + F_j; the last slot gets the given state, which a state written in
+// place may replace before the first segment has read it again.  A workgroup
+// has 16 columns of one head, a wave 16 rows of them.
+__global__ void __launch_bounds__(512) join_kernel(DeltaParams p, int state16) {
+  constexpr int kGroups = kDeltaMaxK / 16;
+  __shared__ float state[kDeltaMaxK][17];
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
+  const int lane = threadIdx.x % 64, m = lane % 16, q = lane / 16;
+  const int vblocks = (p.V + 15) / 16;
+  const int64_t head = blockIdx.x / vblocks;
+  const int h = static_cast<int>(head % p.Hv);
+  const int64_t b = head / p.Hv;
+  const int col = static_cast<int>(blockIdx.x % vblocks) * 16 + m;
+  const int row = 16 * wave + 4 * q;  // the lane's rows of a result: row .. row + 3
+  const int64_t size = static_cast<int64_t>(p.K) * p.V;
+  const auto between = [&](int s) { return p.between + ((b * p.segments + s) * p.Hv + h) * size; };
+  const auto rows_of = [&](const float* at) {
+    float4v v = {};
+#pragma unroll
+    for (int r = 0; r < 4; ++r)
+      if (row + r < p.K && col < p.V) v[r] = at[static_cast<int64_t>(row + r) * p.V + col];
+    return v;
+  };
+  // row 16 wave + m of Phi_j, columns 16 g + 4 q ..
+  const auto phi_of = [&](int j, float4v (&a)[kGroups]) {
+    const float* at = p.phi + ((b * p.segments + j) * p.Hv + h) * static_cast<int64_t>(p.K) * p.K;
+#pragma unroll
+    for (int g = 0; g < kGroups; ++g) {
+      const bool in = 16 * wave + m < p.K && 16 * g + 4 * q < p.K;
+      a[g] = in ? *reinterpret_cast<const float4v*>(&at[(16 * wave + m) * p.K + 16 * g + 4 * q]) : float4v{};
+    }
+  };
+  const auto put = [&](float* at, const float4v& v) {
+#pragma unroll
+    for (int r = 0; r < 4; ++r)
+      if (row + r < p.K && col < p.V) at[static_cast<int64_t>(row + r) * p.V + col] = v[r];
+  };
+  {  // the given state
+    int64_t from = b;
+    bool known = true;
+    if (p.idx != nullptr) {
+      from = p.idx[b];
+      known = from >= 0 && from < p.state_rows;
+    }
+    float4v v = {};
+#pragma unroll
+    for (int r = 0; r < 4; ++r) {
+      const int64_t at = from * p.h0_stride + h * size + static_cast<int64_t>(row + r) * p.V + col;
+      if (!known)
+        v[r] = __builtin_nanf("");
+      else if (p.h0 != nullptr && row + r < p.K && col < p.V)
+        v[r] = state16 ? widen(static_cast<const f16_t*>(p.h0)[at]) : static_cast<const float*>(p.h0)[at];
+    }
+    put(between(p.segments - 1), v);
+  }
+  // Phi and F are asked for two segments ahead
+  struct Segment {
+    float4v f, a[kGroups];
+  } even = {}, odd = {};
+  const auto load = [&](int j, Segment& to) {
+    if (j + 1 >= p.segments) return;
+    to.f = rows_of(between(j));
+    phi_of(j, to.a);
+  };
+  float4v S = rows_of(between(0));
+  const auto step = [&](int j, Segment& seg) {
+#pragma unroll
+    for (int r = 0; r < 4; ++r) state[row + r][m] = S[r];
+    __syncthreads();
+    S = seg.f;
+    float4v more = {};  // two sums, so that a product does not wait for the one before
+#pragma unroll
+    for (int g = 0; g < kGroups; ++g)
+      if (16 * g < p.K)
+#pragma unroll
+        for (int st = 0; st < 4; ++st) {
+          float4v& to = g % 2 ? more : S;
+          to = mfma(seg.a[g][st], state[16 * g + 4 * q + st][m], to);
+        }
+    S += more;
+    put(between(j), S);
+    load(j + 2, seg);
+    __syncthreads();
+  };
+  load(1, odd);
+  load(2, even);
+  for (int j = 1; j + 1 < p.segments; j += 2) {
+    step(j, odd);
+    if (j + 2 < p.segments) step(j + 1, even);
+  }
+}
+
 template <int KP, bool IN32, int OUT, int NV>
 hipError_t launch_typed(const DeltaParams& p, int chain_waves, int state16, hipStream_t s) {
   using Sh = Shared<KP, IN32, OUT>;
   const int width = 16 * NV * chain_waves;
-  const int64_t grid = p.B * p.Hv * ((p.V + width - 1) / width);
+  int64_t grid = p.B * p.Hv * ((p.V + width - 1) / width) * p.segments;
+  if (p.phase == kSegmentEnds) grid = p.B * p.Hv * ((p.V + width - 1) / width + 1) * (p.segments - 1);
   delta_kernel<KP, IN32, OUT, NV>
       <<<dim3(static_cast<uint32_t>(grid)), 64 * (chain_waves + Sh::kPrepare), 0, s>>>(p, chain_waves, state16);
   return hipGetLastError();
@@ -948,21 +1087,36 @@ hipError_t launch_typed(const DeltaParams& p, int chain_waves, int state16, hipS
 
 }  // namespace
 
-hipError_t launch_delta(const DeltaParams& p, int in_dtype, int out_dtype, int state_dtype, int cus, hipStream_t s) {
-  // Columns of a workgroup.  All of a head's (up to 128) where the heads alone
-  // fill the CUs; else fewer, so that more workgroups run the chain of a head.
+hipError_t launch_delta(const DeltaParams& given, int in_dtype, int out_dtype, int state_dtype, int cus, hipStream_t s) {
+  DeltaParams p = given;
+  const int state16 = state_dtype == PRECOG_F16;
+  // Columns of a workgroup: all of a head's, up to 128, or as few as leave every
+  // workgroup a CU of its own (a block takes 3.3 us with 128 columns, 2.3 us with
+  // 32, 1.8 us with 16; two rounds of narrower ones take longer than one).
   int nv = 2, waves = (p.V + 31) / 32;
   if (waves > kChainMax) waves = kChainMax;
-  if (p.B * p.Hv * ((p.V + 32 * waves - 1) / (32 * waves)) < cus) {
-    waves = 1;
-    if (p.B * p.Hv * ((p.V + 31) / 32) < cus) nv = 1;
+  if (p.segments == 1) {
+    const auto fits = [&](int width) { return p.B * p.Hv * ((p.V + width - 1) / width) <= cus; };
+    while (waves > 1 && fits(32 * (waves / 2))) waves /= 2;
+    if (waves == 1 && fits(16)) nv = 1;
   }
-  const int state16 = state_dtype == PRECOG_F16;
   const auto go = [&](auto kp, auto in32, auto out) {
     constexpr int KP = decltype(kp)::value, OUT = decltype(out)::value;
     constexpr bool IN32 = decltype(in32)::value;
-    return nv == 2 ? launch_typed<KP, IN32, OUT, 2>(p, waves, state16, s)
-                   : launch_typed<KP, IN32, OUT, 1>(p, waves, state16, s);
+    if (p.segments == 1) {
+      p.phase = kWhole;
+      return nv == 2 ? launch_typed<KP, IN32, OUT, 2>(p, waves, state16, s)
+                     : launch_typed<KP, IN32, OUT, 1>(p, waves, state16, s);
+    }
+    p.phase = kSegmentEnds;
+    const int phi_waves = (p.K + 31) / 32;
+    hipError_t e = launch_typed<KP, IN32, kNoOutput, 2>(p, waves > phi_waves ? waves : phi_waves, state16, s);
+    if (e != hipSuccess) return e;
+    join_kernel<<<dim3(static_cast<uint32_t>(p.B * p.Hv * ((p.V + 15) / 16))), 64 * ((p.K + 15) / 16), 0, s>>>(p, state16);
+    e = hipGetLastError();
+    if (e != hipSuccess) return e;
+    p.phase = kSegments;
+    return launch_typed<KP, IN32, OUT, 2>(p, waves, state16, s);
   };
   const auto sized = [&](auto in32, auto out) {
     return p.K <= 64 ? go(std::integral_constant<int, 64>{}, in32, out)

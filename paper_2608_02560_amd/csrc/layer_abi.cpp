@@ -84,6 +84,40 @@ precog::DeltaParams delta_params(const precog_delta_desc* d, const void* q, cons
   return p;
 }
 
+// Segments that every sequence of a call is cut into.  A head's blocks of 32
+// tokens run one after the other on one CU, so up to 64 heads leave CUs idle that
+// can take other segments, at three times the work: 8 heads of 40,001 tokens take
+// 2,180 us whole and 380 us in 32 segments, 64 heads of 16,384 tokens 1,180 us
+// and 840 us in 4; 128 heads of 2,048 tokens 162 us and 168 us in 2.  A segment
+// has 16 blocks or more (8 heads of 2,048 tokens: 121 us whole, 100 us in 4).
+int64_t delta_segments(const precog_delta_desc* d, int64_t tokens) {
+  const int64_t heads = d->batch * d->v_heads * ((d->v_dim + 127) / 128);
+  const int64_t blocks = (tokens + 31) / 32 / d->batch;  // of a sequence, on average
+  if (heads > 64) return 1;
+  int64_t n = 256 / heads;
+  if (n > 32) n = 32;
+  if (n > blocks / 16) n = blocks / 16;
+  return n < 4 ? 1 : n;
+}
+
+struct DeltaWs {
+  size_t between, total;
+};
+DeltaWs delta_ws(const precog_delta_desc* d, int64_t segments) {
+  DeltaWs w{0, 0};
+  if (segments <= 1) return w;
+  const size_t rows = static_cast<size_t>(d->batch * segments * d->v_heads * d->k_dim) * 4;
+  w.between = rows * static_cast<size_t>(d->v_dim);
+  w.total = w.between + rows * static_cast<size_t>(d->k_dim);
+  return w;
+}
+
+// Tokens of a call, or -1 if there are more than a call can have.
+int64_t delta_tokens(int64_t B, int64_t L, bool packed) {
+  if (packed) return L;
+  return L > 0 && B > kMaxTokens / L ? -1 : B * L;
+}
+
 precog_status validate_conv(const precog_conv_desc* d, bool step) {
   if (!d) return PRECOG_ERR_NULL;
   if (d->batch < 0 || d->dim < 0 || (!step && d->seqlen < 0)) return PRECOG_ERR_SHAPE;
@@ -147,14 +181,22 @@ ScoreWs score_ws(int64_t T, int64_t splits, int64_t top) {
 
 extern "C" {
 
+size_t precog_delta_workspace_bytes(const precog_delta_desc* desc, int packed) {
+  if (validate_delta(desc, false) != PRECOG_OK) return 0;
+  const int64_t tokens = delta_tokens(desc->batch, desc->seqlen, packed != 0);
+  if (tokens <= 0 || desc->batch == 0 || desc->batch * desc->v_heads > kMaxTokens / 8) return 0;
+  return delta_ws(desc, delta_segments(desc, tokens)).total;
+}
+
 precog_status precog_delta_encode(const precog_delta_desc* desc, const void* q, const void* k,
                                   const void* v, const float* g, const float* beta,
                                   const int32_t* starts, const void* h0, int64_t h0_rows,
-                                  const int32_t* h0_idx, void* o, void* hT, void* stream) {
+                                  const int32_t* h0_idx, void* o, void* hT, void* workspace,
+                                  size_t workspace_bytes, void* stream) {
   precog_status st = validate_delta(desc, false);
   if (st != PRECOG_OK) return st;
   const int64_t B = desc->batch, L = desc->seqlen;
-  const int64_t tokens = starts ? L : (L > 0 && B > kMaxTokens / L ? -1 : B * L);
+  const int64_t tokens = delta_tokens(B, L, starts != nullptr);
   if (tokens < 0) return PRECOG_ERR_SHAPE;
   if (B * desc->v_heads > kMaxTokens / 8) return PRECOG_ERR_SHAPE;  // workgroups, 8 a head at most
   if (B == 0) return PRECOG_OK;
@@ -163,7 +205,8 @@ precog_status precog_delta_encode(const precog_delta_desc* desc, const void* q, 
   if ((!o || !work) && !hT) return PRECOG_OK;  // nothing requested
   if (h0_idx && h0_rows < 0) return PRECOG_ERR_SHAPE;
   if (h0_idx && h0_rows > 0 && !h0) return PRECOG_ERR_NULL;
-  for (const void* p : {q, k, v, h0, static_cast<const void*>(o), static_cast<const void*>(hT)})
+  for (const void* p : {q, k, v, h0, static_cast<const void*>(o), static_cast<const void*>(hT),
+                        static_cast<const void*>(workspace)})
     if (!aligned(p, 16)) return PRECOG_ERR_ALIGN;
   if (!aligned(g, 4) || !aligned(beta, 4) || !aligned(starts, 4) || !aligned(h0_idx, 4))
     return PRECOG_ERR_ALIGN;
@@ -187,6 +230,13 @@ precog_status precog_delta_encode(const precog_delta_desc* desc, const void* q, 
     const size_t pitch = static_cast<size_t>(p.h0_stride) * es, one = static_cast<size_t>(sd) * es;
     const size_t off = (a < b ? b - a : a - b) % pitch;
     if (!layers || (h0 != hT && (off < one || off + one > pitch))) return PRECOG_ERR_STRIDE;
+  }
+  p.segments = static_cast<int>(work ? delta_segments(desc, tokens) : 1);
+  const DeltaWs ws = delta_ws(desc, p.segments);
+  if (ws.total > 0 && (!workspace || workspace_bytes < ws.total)) return PRECOG_ERR_WORKSPACE;
+  if (ws.total > 0) {
+    p.between = static_cast<float*>(workspace);
+    p.phi = reinterpret_cast<float*>(static_cast<char*>(workspace) + ws.between);
   }
   int cus = 1;
   st = precog::check_device(&cus);
@@ -230,7 +280,7 @@ precog_status precog_conv_encode(const precog_conv_desc* desc, const void* x, co
   precog_status st = validate_conv(desc, false);
   if (st != PRECOG_OK) return st;
   const int64_t B = desc->batch, L = desc->seqlen, D = desc->dim;
-  const int64_t tokens = starts ? L : (L > 0 && B > kMaxTokens / L ? -1 : B * L);
+  const int64_t tokens = delta_tokens(B, L, starts != nullptr);
   if (tokens < 0) return PRECOG_ERR_SHAPE;
   if (B == 0 || D == 0) return PRECOG_OK;
   const bool work = tokens > 0;

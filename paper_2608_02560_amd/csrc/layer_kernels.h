@@ -30,7 +30,12 @@ struct DeltaParams {
   int Hk, Hv, K, V;
   int norm;
   float eps, scale;
+  int segments;            // of every sequence, 1: whole
+  int phase;               // one of the following, set by launch_delta
+  float* between;          // [B, segments, Hv, K, V] (workspace), segments > 1 only
+  float* phi;              // [B, segments, Hv, K, K] (workspace)
 };
+constexpr int kWhole = 0, kSegmentEnds = 1, kSegments = 2;
 hipError_t launch_delta(const DeltaParams& p, int in_dtype, int out_dtype, int state_dtype, int cus,
                         hipStream_t s);
 hipError_t launch_delta_step(const DeltaParams& p, int in_dtype, int out_dtype, int state_dtype,

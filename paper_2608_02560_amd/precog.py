@@ -34,7 +34,8 @@ EXPORTS = ("precog_scan_workspace_bytes", "precog_scan_encode", "precog_scan_enc
            "precog_retrieve_topk_prepared", "precog_query_workspace_bytes",
            "precog_query_top1_prefill", "precog_inject_gather", "precog_inject_compose",
            "precog_inject_fuse",
-           "precog_smc_route", "precog_smc_consolidate", "precog_delta_encode",
+           "precog_smc_route", "precog_smc_consolidate", "precog_delta_workspace_bytes",
+           "precog_delta_encode",
            "precog_delta_step", "precog_conv_encode", "precog_conv_step",
            "precog_score_workspace_bytes", "precog_score_tokens", "precog_status_string")
 
@@ -133,7 +134,10 @@ def lib():
         L.precog_smc_consolidate.argtypes = [vp, ctypes.c_int, i64, i64, vp, ctypes.c_int, vp, i64,
                                              ctypes.c_double, vp]
         L.precog_smc_consolidate.restype = ctypes.c_int
-        L.precog_delta_encode.argtypes = [ctypes.POINTER(DeltaDesc)] + [vp] * 7 + [i64] + [vp] * 4
+        L.precog_delta_workspace_bytes.argtypes = [ctypes.POINTER(DeltaDesc), ctypes.c_int]
+        L.precog_delta_workspace_bytes.restype = sz
+        L.precog_delta_encode.argtypes = [ctypes.POINTER(DeltaDesc)] + [vp] * 7 + [i64] + [vp] * 4 + \
+            [sz, vp]
         L.precog_delta_encode.restype = ctypes.c_int
         L.precog_delta_step.argtypes = [ctypes.POINTER(DeltaDesc)] + [vp] * 6 + [i64] + [vp] * 3
         L.precog_delta_step.restype = ctypes.c_int
@@ -389,12 +393,17 @@ def delta_desc(batch, seqlen, k_heads, v_heads, k_dim, v_dim, in_dtype=BF16, out
                      1 if qk_norm else 0, eps, scale)
 
 
+def delta_workspace_bytes(desc: DeltaDesc, packed=False) -> int:
+    return int(lib().precog_delta_workspace_bytes(ctypes.byref(desc), int(bool(packed))))
+
+
 def delta_encode(desc: DeltaDesc, q, k, v, g=None, beta=None, starts=None, h0=None, h0_rows=0,
-                 h0_idx=None, o=None, hT=None, stream=None):
+                 h0_idx=None, o=None, hT=None, workspace=None, workspace_bytes=0, stream=None):
     """precog_delta_encode on device tensors (or raw device pointers)."""
     st = lib().precog_delta_encode(ctypes.byref(desc), _ptr(q), _ptr(k), _ptr(v), _ptr(g),
                                    _ptr(beta), _ptr(starts), _ptr(h0), int(h0_rows), _ptr(h0_idx),
-                                   _ptr(o), _ptr(hT), _stream(stream))
+                                   _ptr(o), _ptr(hT), _ptr(workspace), int(workspace_bytes),
+                                   _stream(stream))
     _check("precog_delta_encode", st)
 
 
@@ -728,8 +737,10 @@ def delta(q, k, v, g=None, beta=None, h0=None, *, starts=None, h0_idx=None, qk_n
         o = torch.empty(tuple(v.shape), dtype=out_dtype, device=dev) if want_o else None
         if want_hT and hT is None:
             hT = torch.empty((B, Hv, K, V), dtype=state_dtype, device=dev)
+        nbytes = delta_workspace_bytes(desc, starts is not None)
+        ws = torch.empty(nbytes, dtype=torch.uint8, device=dev) if nbytes else None
     delta_encode(desc, q, k, v, g, beta, starts, h0, h0.shape[0] if h0 is not None else 0, h0_idx,
-                 o, hT, stream)
+                 o, hT, ws, nbytes, stream)
     return o, hT
 
 

@@ -53,7 +53,8 @@ int main() {
           d.*a = x;
           d.*b = y;
           const precog_status s = precog_delta_encode(&d, q, at(0x20000), at(0x30000), f, f, nullptr, at(0x40000),
-                                                      x, nullptr, at(0x50000), at(0x60000), nullptr);
+                                                      x, nullptr, at(0x50000), at(0x60000), nullptr, 0, nullptr);
+          precog_delta_workspace_bytes(&d, static_cast<int>(x & 1));
           CHECK(refused(s) || d.batch == 0);
           const precog_status t = precog_delta_step(&d, q, at(0x20000), at(0x30000), f, f, at(0x40000), 4,
                                                     static_cast<int32_t*>(at(0x1000)), at(0x50000), nullptr);
@@ -63,12 +64,12 @@ int main() {
   for (uintptr_t h0 : {uintptr_t{0x100000}, ~uintptr_t{0xfffff}})
     for (uintptr_t hT : {uintptr_t{0x100010}, ~uintptr_t{0xfffef}, uintptr_t{0x110000}})
       precog_delta_encode(&good, q, at(0x20000), at(0x30000), f, f, nullptr, at(h0), 2, nullptr, at(0x50000), at(hT),
-                          nullptr);
-  CHECK(precog_delta_encode(nullptr, q, q, q, f, f, nullptr, q, 0, nullptr, q, q, nullptr) == PRECOG_ERR_NULL);
+                          nullptr, 0, nullptr);
+  CHECK(precog_delta_encode(nullptr, q, q, q, f, f, nullptr, q, 0, nullptr, q, q, nullptr, 0, nullptr) == PRECOG_ERR_NULL);
   for (float v : {-1.f, std::nanf(""), INFINITY}) {
     precog_delta_desc d = good;
     d.eps = v;
-    CHECK(refused(precog_delta_encode(&d, q, q, q, f, f, nullptr, q, 0, nullptr, q, q, nullptr)));
+    CHECK(refused(precog_delta_encode(&d, q, q, q, f, f, nullptr, q, 0, nullptr, q, q, nullptr, 0, nullptr)));
   }
 
   precog_conv_desc conv{2, 16, 64, 4, 0, PRECOG_BF16, PRECOG_F32, 1};

@@ -247,6 +247,52 @@ def test_long_sequence():
     _run([2500], 1, 1, 64, 32, torch.bfloat16, torch.bfloat16, torch.float32)
 
 
+@pytest.mark.parametrize("lens,K,V,st", [
+    ([2111], 64, 48, torch.float32),                    # segments of unequal length
+    ([2048 + 32], 128, 200, torch.float16),             # two column blocks a segment
+    ([0, 40000, 1, 31, 33, 0, 700, 65], 40, 72, torch.float32),  # some shorter than their segments
+    ([6000, 5999], 96, 128, torch.float32)])
+@pytest.mark.parametrize("h0", [True, False])
+def test_segments(lens, K, V, st, h0):
+    """Few heads of long sequences are cut in time."""
+    Hk, Hv = 1, 2
+    desc = P.delta_desc(len(lens), sum(lens), Hk, Hv, K, V)
+    assert P.delta_workspace_bytes(desc, True) > 0
+    _run(lens, Hk, Hv, K, V, torch.bfloat16, torch.float32, st, h0=h0)
+
+
+def test_segments_in_place_and_from_a_store():
+    lens, Hv, K, V = [2500, 3100], 2, 64, 64
+    d = delta_inputs(sum(lens), 1, Hv, K, V, 70)
+    c, s = on_gpu(d), starts_of(lens).to(DEV)
+    h0 = _states(2, Hv, K, V, torch.float32, 71)
+    ro, rS = delta_oracle(d, lens, h0, qk_norm=True)
+    state = h0.to(DEV)
+    o, _ = P.delta(c["q"], c["k"], c["v"], c["g"], c["beta"], state, starts=s, qk_norm=True, hT=state)
+    check(o, ro, delta_bar(3100))
+    check(state, rS, delta_bar(3100))
+    store = torch.zeros((5, Hv, K, V), device=DEV)
+    store[3], store[0] = h0[0].to(DEV), h0[1].to(DEV)
+    idx = torch.tensor([3, 0], dtype=torch.int32, device=DEV)
+    o2, hT = P.delta(c["q"], c["k"], c["v"], c["g"], c["beta"], store, starts=s, h0_idx=idx, qk_norm=True)
+    assert torch.equal(o, o2) and torch.equal(state, hT)
+    idx = torch.tensor([3, 5], dtype=torch.int32, device=DEV)
+    o3, hT = P.delta(c["q"], c["k"], c["v"], c["g"], c["beta"], store, starts=s, h0_idx=idx, qk_norm=True)
+    assert torch.equal(o3[:2500], o[:2500]) and torch.isnan(o3[2500:]).all() and torch.isnan(hT[1]).all()
+
+
+def test_segments_with_resets():
+    """Log decays that empty the state inside a segment and at its edges."""
+    d = delta_inputs(2200, 1, 1, 64, 64, 72)
+    d["g"][::64] = -np.inf
+    d["g"][1111:1190] = -5.0
+    c = on_gpu(d)
+    o, hT = P.delta(c["q"], c["k"], c["v"], c["g"], c["beta"], starts=starts_of([2200]).to(DEV), qk_norm=True)
+    ro, rS = delta_oracle(d, [2200], qk_norm=True)
+    check(o, ro, delta_bar(2200))
+    check(hT, rS, delta_bar(2200))
+
+
 def test_two_runs_are_bitwise_equal():
     d = on_gpu(delta_inputs(400, 2, 4, 128, 128, 20))
     s = starts_of([150, 250]).to(DEV)

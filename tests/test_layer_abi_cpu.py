@@ -15,8 +15,8 @@ def _ref(d):
 
 
 def _delta(desc, q=FAKE, k=FAKE, v=FAKE, g=FAKE, beta=FAKE, starts=None, h0=None, rows=0, idx=None, o=FAKE,
-           hT=FAKE + 0x100000):
-    return P.lib().precog_delta_encode(_ref(desc), q, k, v, g, beta, starts, h0, rows, idx, o, hT, None)
+           hT=FAKE + 0x100000, ws=None, nbytes=0):
+    return P.lib().precog_delta_encode(_ref(desc), q, k, v, g, beta, starts, h0, rows, idx, o, hT, ws, nbytes, None)
 
 
 def _step(desc, q=FAKE, k=FAKE, v=FAKE, g=FAKE, beta=FAKE, states=FAKE, rows=4, slots=FAKE, o=FAKE):
@@ -74,6 +74,19 @@ def test_delta_arguments():
     assert _delta(good, h0=FAKE, hT=FAKE + 16) == ESTRIDE
     layers = P.delta_desc(2, 16, 2, 4, 64, 64, h0_batch_stride=3 * 4 * 64 * 64, hT_batch_stride=3 * 4 * 64 * 64)
     assert _delta(layers, h0=FAKE, hT=FAKE + row // 2) == ESTRIDE
+
+
+def test_delta_workspace():
+    long = P.delta_desc(1, 40000, 2, 4, 128, 128)
+    need = P.delta_workspace_bytes(long)
+    assert need > 0 and need == P.delta_workspace_bytes(long, True)
+    assert _delta(long) == EWS and _delta(long, ws=FAKE, nbytes=need - 1) == EWS
+    assert _delta(long, ws=FAKE + 8, nbytes=need) == EALIGN
+    for d in (P.delta_desc(2, 16, 2, 4, 64, 64), P.delta_desc(0, 40000, 2, 4, 64, 64),
+              P.delta_desc(64, 40000, 2, 4, 64, 64), P.delta_desc(1, 40000, 2, 3, 64, 64),
+              P.delta_desc(1, 40000, 33, 66, 64, 64), P.delta_desc(1, 2000, 2, 4, 64, 64),
+              P.delta_desc(1 << 20, 1 << 20, 1, 1, 64, 64)):
+        assert P.delta_workspace_bytes(d) == 0
 
 
 def test_nothing_to_do_is_ok_without_a_gpu():

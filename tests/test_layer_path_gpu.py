@@ -7,7 +7,7 @@ import pytest
 import torch
 
 import oracle
-from layer_testutil import check, delta_bar, starts_of
+from layer_testutil import O16, check, delta_bar, starts_of
 from paper_2608_02560_amd import precog as P
 
 pytestmark = pytest.mark.gpu
@@ -283,7 +283,9 @@ def test_offsets_past_32_bits():
     a = P.delta(q, k, v, gates, None, starts=starts, qk_norm=True, out_dtype=torch.bfloat16)
     q, k, v = _split(x[T - 70:].clone())
     b = P.delta(q, k, v, gates[:70], None, starts=starts_of([40, 30]).to(DEV), qk_norm=True, out_dtype=torch.bfloat16)
-    assert torch.equal(a[0][T - 70:], b[0]) and torch.equal(a[1], b[1])
+    # the many tokens have the first call computed in segments: equal but for rounding
+    check(a[0][T - 70:], b[0].double().cpu().numpy(), O16)
+    check(a[1], b[1].double().cpu().numpy(), 2 * delta_bar(40))
     cw = torch.randn((D, 4), device=DEV)
     a = P.conv(x, cw, starts=starts)
     b = P.conv(x[T - 70:].clone(), cw, starts=starts_of([40, 30]).to(DEV))
