@@ -985,39 +985,50 @@ __global__ void __launch_bounds__(64 * (kChainMax + Shared<KP, IN32, OUT>::kPrep
 // Phi_j S + F_j; the last slot gets the given state, which a state written in
 // place may replace before the first segment has read it again.  A workgroup
 // has 16 columns of one head, a wave 16 rows of them.
-__global__ void __launch_bounds__(512) join_kernel(DeltaParams p, int state16) {
-  constexpr int kGroups = kDeltaMaxK / 16;
-  __shared__ float state[kDeltaMaxK][17];
+template <int KP>
+__global__ void __launch_bounds__(4 * KP) join_kernel(DeltaParams p, int state16) {
+  constexpr int kGroups = KP / 16;
+  __shared__ float state[KP][17];
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
   const int lane = threadIdx.x % 64, m = lane % 16, q = lane / 16;
   const int vblocks = (p.V + 15) / 16;
-  const int64_t head = blockIdx.x / vblocks;
-  const int h = static_cast<int>(head % p.Hv);
+  const int at_block = xcd_remap(blockIdx.x, gridDim.x);  // a head's columns read one Phi
+  const int head = at_block / vblocks;
+  const int h = head % p.Hv;
   const int64_t b = head / p.Hv;
-  const int col = static_cast<int>(blockIdx.x % vblocks) * 16 + m;
+  const int col = at_block % vblocks * 16 + m;
   const int row = 16 * wave + 4 * q;  // the lane's rows of a result: row .. row + 3
   const int64_t size = static_cast<int64_t>(p.K) * p.V;
   const auto between = [&](int s) { return p.between + ((b * p.segments + s) * p.Hv + h) * size; };
+  // rows from K on and columns from V on lie past a buffer's end: read as zeros,
+  // not written
+  const uint32_t f_off = col < p.V ? static_cast<uint32_t>(row * p.V + col) * 4 : kDropOffset;
   const auto rows_of = [&](const float* at) {
-    float4v v = {};
+    const __amdgpu_buffer_rsrc_t buf = make_rsrc(at, static_cast<uint32_t>(size) * 4);
+    float4v v;
 #pragma unroll
     for (int r = 0; r < 4; ++r)
-      if (row + r < p.K && col < p.V) v[r] = at[static_cast<int64_t>(row + r) * p.V + col];
+      v[r] = __uint_as_float(
+          __builtin_bit_cast(uint32_t, __builtin_amdgcn_raw_buffer_load_b32(buf, f_off + 4 * r * p.V, 0, 0)));
     return v;
   };
   // row 16 wave + m of Phi_j, columns 16 g + 4 q ..
   const auto phi_of = [&](int j, float4v (&a)[kGroups]) {
-    const float* at = p.phi + ((b * p.segments + j) * p.Hv + h) * static_cast<int64_t>(p.K) * p.K;
+    const __amdgpu_buffer_rsrc_t buf =
+        make_rsrc(p.phi + ((b * p.segments + j) * p.Hv + h) * static_cast<int64_t>(p.K) * p.K,
+                  static_cast<uint32_t>(p.K * p.K) * 4);
 #pragma unroll
     for (int g = 0; g < kGroups; ++g) {
-      const bool in = 16 * wave + m < p.K && 16 * g + 4 * q < p.K;
-      a[g] = in ? *reinterpret_cast<const float4v*>(&at[(16 * wave + m) * p.K + 16 * g + 4 * q]) : float4v{};
+      const int c = 16 * g + 4 * q;
+      const uint32_t off = c < p.K ? static_cast<uint32_t>((16 * wave + m) * p.K + c) * 4 : kDropOffset;
+      a[g] = __builtin_bit_cast(float4v, __builtin_amdgcn_raw_buffer_load_b128(buf, off, 0, 0));
     }
   };
   const auto put = [&](float* at, const float4v& v) {
+    const __amdgpu_buffer_rsrc_t buf = make_rsrc(at, static_cast<uint32_t>(size) * 4);
 #pragma unroll
     for (int r = 0; r < 4; ++r)
-      if (row + r < p.K && col < p.V) at[static_cast<int64_t>(row + r) * p.V + col] = v[r];
+      __builtin_amdgcn_raw_buffer_store_b32(__float_as_uint(v[r]), buf, f_off + 4 * r * p.V, 0, 0);
   };
   {  // the given state
     int64_t from = b;
@@ -1055,12 +1066,11 @@ __global__ void __launch_bounds__(512) join_kernel(DeltaParams p, int state16) {
     float4v more = {};  // two sums, so that a product does not wait for the one before
 #pragma unroll
     for (int g = 0; g < kGroups; ++g)
-      if (16 * g < p.K)
 #pragma unroll
-        for (int st = 0; st < 4; ++st) {
-          float4v& to = g % 2 ? more : S;
-          to = mfma(seg.a[g][st], state[16 * g + 4 * q + st][m], to);
-        }
+      for (int st = 0; st < 4; ++st) {
+        float4v& to = g % 2 ? more : S;
+        to = mfma(seg.a[g][st], state[16 * g + 4 * q + st][m], to);
+      }
     S += more;
     put(between(j), S);
     load(j + 2, seg);
@@ -1112,7 +1122,7 @@ hipError_t launch_delta(const DeltaParams& given, int in_dtype, int out_dtype, i
     const int phi_waves = (p.K + 31) / 32;
     hipError_t e = launch_typed<KP, IN32, kNoOutput, 2>(p, waves > phi_waves ? waves : phi_waves, state16, s);
     if (e != hipSuccess) return e;
-    join_kernel<<<dim3(static_cast<uint32_t>(p.B * p.Hv * ((p.V + 15) / 16))), 64 * ((p.K + 15) / 16), 0, s>>>(p, state16);
+    join_kernel<KP><<<dim3(static_cast<uint32_t>(p.B * p.Hv * ((p.V + 15) / 16))), 4 * KP, 0, s>>>(p, state16);
     e = hipGetLastError();
     if (e != hipSuccess) return e;
     p.phase = kSegments;
