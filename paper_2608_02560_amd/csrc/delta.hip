@@ -111,7 +111,7 @@ __device__ __forceinline__ int a_at(int row, int col) { return 32 * row + 4 * (c
 template <int KP, bool IN32, int OUT>
 struct Shared {
   // as many as fit into the 160 KB of a CU, up to five
-  static constexpr int kBuffers = IN32 ? 2 : KP == 128 && OUT == kOut32 ? 4 : 5;
+  static constexpr int kBuffers = IN32 ? (KP == 128 ? 2 : 4) : KP == 128 && OUT == kOut32 ? 4 : 5;
   static constexpr int kPrepare = kBuffers - 1;   // prepare waves: each works on a buffer of its own
   Buffer<KP, IN32, OUT> buf[kBuffers];
   Scratch scratch[kPrepare];
