@@ -582,8 +582,11 @@ size_t precog_delta_workspace_bytes(const precog_delta_desc *desc, int packed);
  *              (then q is not read and may be NULL).
  *   hT         state rows like h0, or NULL.  May equal h0 exactly without
  *              h0_idx (in place); must not overlap h0 otherwise.
- * Arithmetic in fp32.  A NaN or an infinity in a token reaches o of its head
- * and sequence from the beginning of the token's block of 32 on.
+ * Arithmetic: states, sums, decays and norms in fp32; the products of blocks
+ * of 32 tokens run on the matrix cores with operands of 22 bits (11 bits for
+ * what only enters a bf16 o).  With norms of 2^63 and more the sum of squares
+ * leaves fp32.  A NaN or an infinity in a token reaches o of its head and
+ * sequence from the beginning of the token's block of 32 on.
  *   workspace  precog_delta_workspace_bytes(desc, starts != NULL) bytes; NULL
  *              where that is 0.
  * Alignment: pointers 16 bytes (g, beta, starts, h0_idx: 4), strides as above.
