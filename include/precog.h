@@ -584,11 +584,13 @@ size_t precog_delta_workspace_bytes(const precog_delta_desc *desc, int packed);
  *              h0_idx (in place); must not overlap h0 otherwise.
  * Arithmetic: states, sums, decays and norms in fp32; the products of blocks
  * of 32 tokens run on the matrix cores with operands of 22 bits (11 bits for
- * what only enters a bf16 o).  With norms of 2^63 and more the sum of squares
+ * what only enters a bf16 o), counted from the largest of a column and block:
+ * where beta |k|^2 > 2 lets the rule expand, a block's small results are good
+ * to 2^-20 of its large ones.  With norms of 2^63 and more the sum of squares
  * leaves fp32.  A NaN or an infinity in a token reaches o of its head and
  * sequence from the beginning of the token's block of 32 on.
  *   workspace  precog_delta_workspace_bytes(desc, starts != NULL) bytes; NULL
- *              where that is 0.
+ *              where that is 0.  Calls that may overlap need one each.
  * Alignment: pointers 16 bytes (g, beta, starts, h0_idx: 4), strides as above.
  * Deterministic; nothing but o, hT and the workspace is written. */
 precog_status precog_delta_encode(const precog_delta_desc *desc, const void *q,
@@ -687,7 +689,8 @@ size_t precog_score_workspace_bytes(int64_t T, int64_t V, int64_t top);
  * alternatives beyond the unmasked ones have id -1 and -infinity.  A row with
  * nothing unmasked has logprob -infinity and entropy 0.  A row with a NaN or a
  * +infinity has NaN in all its numbers and ids of -1.  Sums in fp32.
- *   workspace  precog_score_workspace_bytes(T, V, top) bytes
+ *   workspace  precog_score_workspace_bytes(T, V, top) bytes; calls that may
+ *              overlap need one each
  * T < 2^31, V <= 2^28; logits aligned as their type, workspace 16 bytes, others 4. */
 precog_status precog_score_tokens(const void *logits, precog_dtype logits_dtype,
                                   int64_t T, int64_t V, int64_t row_stride,

@@ -161,7 +161,8 @@ __device__ __forceinline__ Scale scale_of(float m) {
   return {__uint_as_float(static_cast<uint32_t>(268 - e) << 23), __uint_as_float(static_cast<uint32_t>(e - 14) << 23)};
 }
 
-// x - h[i], in one instruction.
+// x - h[i], in one instruction.  x may come straight from a matrix instruction:
+// the conversion that made h has read it before, and has waited for it.
 template <int I>
 __device__ __forceinline__ float less_half(float x, half2 h) {
   float d;
@@ -787,7 +788,8 @@ __global__ void __launch_bounds__(64 * (kChainMax + Shared<KP, IN32, OUT>::kPrep
 #pragma unroll
   for (int n = 0; n < NV; ++n) {
     const float most = largest(n);
-    const Scale sc = scale_of(most);
+    // (a sequence without tokens hands its state on bit for bit)
+    const Scale sc = blocks > 0 ? scale_of(most) : Scale{1.f, 1.f};
     sigma[n] = sc.down;
     bound[n] = most * sc.up;
 #pragma unroll

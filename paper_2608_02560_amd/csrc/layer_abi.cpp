@@ -121,7 +121,7 @@ int64_t delta_tokens(int64_t B, int64_t L, bool packed) {
 precog_status validate_conv(const precog_conv_desc* d, bool step) {
   if (!d) return PRECOG_ERR_NULL;
   if (d->batch < 0 || d->dim < 0 || (!step && d->seqlen < 0)) return PRECOG_ERR_SHAPE;
-  if (d->batch > kMaxTokens || d->dim > kMaxStride || (!step && d->seqlen > kMaxTokens))
+  if (d->batch > (1LL << 30) || d->dim > kMaxStride || (!step && d->seqlen > kMaxTokens))
     return PRECOG_ERR_SHAPE;
   if (step && d->batch > 65535) return PRECOG_ERR_SHAPE;
   if (d->width < 2 || d->width > 4) return PRECOG_ERR_SHAPE;

@@ -841,6 +841,8 @@ def score_tokens(logits, token=None, top=0, *, want_entropy=True, stream=None):
     stride = logits.stride(0) if T > 1 else V
     if stride < V:
         raise ValueError("logits: rows must not overlap")
+    if not 0 <= top <= 64:
+        raise ValueError("top must be 0..64, not %d" % top)
     if token is not None:
         _same("token", token, torch.int32, (T,), dev)
     nbytes = score_workspace_bytes(T, V, top)

@@ -160,6 +160,37 @@ def test_rows_outside_the_sequences_stay():
     assert (hT[1] == 0).all()
 
 
+def test_empty_sequences_hand_their_state_on():
+    """Bit for bit, infinities, NaN and tiny numbers among them; no sequences at all is no call."""
+    h0 = torch.randn((3, 2, 64, 64), device=DEV)
+    h0[0, 0, 3, 5], h0[0, 1, 4, 6], h0[1, 0, 0, 0], h0[1, 0, 1, 0] = np.inf, np.nan, 1e-41, 1e30
+    d = on_gpu(delta_inputs(5, 1, 2, 64, 64, 21))
+    zero = {n: t[:0] for n, t in d.items()}
+    for p in (zero, d):
+        starts = torch.full((4,), 0 if p is zero else 2, dtype=torch.int32, device=DEV)
+        _, hT = P.delta(p["q"], p["k"], p["v"], p["g"], p["beta"], h0, starts=starts)
+        assert torch.equal(hT.view(torch.int32), h0.view(torch.int32))
+    o, hT = P.delta(d["q"], d["k"], d["v"], d["g"], d["beta"], starts=starts[:1])
+    assert o.shape == (5, 2, 64) and hT.shape == (0, 2, 64, 64)
+
+
+@pytest.mark.parametrize("beta", [1.0, 2.0])
+def test_reflecting_keys(beta):
+    """beta up to 2 (eigenvalues down to -1) and keys that resemble one another."""
+    d = delta_inputs(200, 1, 2, 64, 64, 22)
+    d["k"] = (d["k"].float() * 0.3 + torch.randn(64, generator=torch.Generator().manual_seed(23))).bfloat16()
+    d["beta"][:] = beta
+    d["g"] = d["g"] * 0.01
+    c = on_gpu(d)
+    o, hT = P.delta(c["q"], c["k"], c["v"], c["g"], c["beta"], starts=starts_of([200]).to(DEV), qk_norm=True)
+    ro, rS = delta_oracle(d, [200], qk_norm=True)
+    # beyond beta = 1 the inverse grows with the sum of the block's reflections:
+    # entries up to 2 a token pair, sums of 32 of them
+    bar = delta_bar(200) * (1 if beta <= 1 else 8)
+    check(o, ro, bar)
+    check(hT, rS, bar)
+
+
 def test_bad_starts_are_clamped():
     T = 40
     d = on_gpu(delta_inputs(T, 1, 1, 64, 64, 14))

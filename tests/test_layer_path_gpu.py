@@ -328,5 +328,6 @@ def test_refusals_of_the_wrappers():
     bad(lambda: P.score_tokens(t["x"], t["token"].long()))
     bad(lambda: P.score_tokens(t["x"], t["token"][:3]))
     bad(lambda: P.score_tokens(t["x"], t["token"], top=65))
+    bad(lambda: P.score_tokens(t["x"], t["token"], top=-1))
     bad(lambda: P.score_tokens(t["x"].t(), None, top=1))
     bad(lambda: P.score_tokens(t["x"][:1].expand(6, D), t["token"]))
