@@ -670,10 +670,13 @@ def _token_stride(name, t, lead):
     return stride
 
 
+_CURRENT_STREAM = contextlib.nullcontext()
+
+
 def _own_stream(stream):
     """Context in which torch allocates from the stream that the kernels run on."""
     if stream is None:
-        return contextlib.nullcontext()
+        return _CURRENT_STREAM
     return torch.cuda.stream(torch.cuda.ExternalStream(stream) if isinstance(stream, int)
                              else stream)
 

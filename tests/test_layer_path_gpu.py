@@ -202,6 +202,41 @@ def test_prefill_graph_replays_equal_eager():
             assert torch.equal(a[:n], b[:n])
 
 
+def test_segmented_prefill_graph_replays_equal_eager():
+    """A long sequence in time segments, captured with its workspace; two graphs
+    of it side by side."""
+    lens = [2300, 1900]
+    sets = [_dev(_tokens(sum(lens), 90 + i)) for i in range(3)]
+    starts = starts_of(lens).to(DEV)
+    static = [{n: t.clone() for n, t in sets[0].items()} for _ in range(2)]
+
+    def run(t):
+        q, k, v = _split(t["x"])
+        return P.delta(q, k, v, t["g"], t["beta"], starts=starts, qk_norm=True, out_dtype=torch.bfloat16)
+
+    run(static[0])
+    graphs, outs = [], []
+    for s in static:
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g):
+            outs.append(run(s))
+        graphs.append(g)
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    for rep in range(4):
+        pick = [sets[(rep + i) % 3] for i in range(2)]
+        for s, t in zip(static, pick):
+            for n in s:
+                s[n].copy_(t[n])
+        eager = [run(t) for t in pick]
+        torch.cuda.synchronize()
+        for g, s in zip(graphs, streams):
+            with torch.cuda.stream(s):
+                g.replay()
+        torch.cuda.synchronize()
+        for a, b in zip(outs, eager):
+            assert torch.equal(a[0], b[0]) and torch.equal(a[1], b[1])
+
+
 @pytest.mark.parametrize("as_int", [False, True])
 def test_other_streams(as_int):
     """Two streams at once, named by argument, while the current one is neither."""
