@@ -32,11 +32,17 @@
 // fp64, where the differences of two positions are taken).  A product's
 // operands are fp16: keys and queries under the power of two that brings the
 // row's norm to [1, 2) (exact for bf16 down to 2^-16 of it, good to 2^-25; fp32
-// inputs as two halves of 11 bits), and S,
-// X, U and T as two halves (22 bits) under a power of two that puts their
-// column's (T: block's) largest at 2^14, so neither half runs out of range.
-// Products of two low halves are left out (2^-22).  What only enters a bf16 o
-// (Q S, Q K^T U) takes the high halves alone: 2^-11 against the 2^-8 of o.
+// inputs as two halves of 11 bits), and S, X, U and T as two halves (22 bits)
+// under a power of two of their own, a column's (T: a block's): X and T have
+// their largest at 2^14, S and U are held below 2^16 and 2^8 by bounds that are
+// known before they are.  Products of two low halves are left out (2^-22).  What
+// only enters a bf16 o (Q S, Q K^T U) takes the high halves alone: 2^-11 against
+// the 2^-8 of o.  Errors against 64 bits over 40,001 tokens: states 2.2e-7, as a
+// plain evaluation in 32 bits; two bf16 halves would leave 3e-6.
+//
+// What bounds it: vector instructions (65 % of the issue slots, beside 25 % for
+// the matrix ones, at 32 sequences of 3,000 tokens and 16 heads of 128 x 128:
+// 540 us, 2.2 TB/s).
 //
 // Long sequences of few heads.  A head's blocks follow one another, so a call of
 // fewer heads than CUs is cut into segments of each sequence: the end state of a

@@ -681,6 +681,14 @@ def _own_stream(stream):
                              else stream)
 
 
+def _at(t):
+    return None if t is None else t.data_ptr()
+
+
+def _handle(stream, device):
+    return torch._C._cuda_getCurrentRawStream(device) if stream is None else _stream(stream)
+
+
 def _delta_args(q, k, v, g, beta, lead, out_dtype, state_dtype):
     dev = _device_of(k)
     if k.dim() != lead + 2 or v.dim() != lead + 2:
@@ -735,15 +743,18 @@ def delta(q, k, v, g=None, beta=None, h0=None, *, starts=None, h0_idx=None, qk_n
         _same("h0", h0, state_dtype, (rows, Hv, K, V), dev)
     if hT is not None:
         _same("hT", hT, state_dtype, (B, Hv, K, V), dev)
-    desc = delta_desc(B, L, Hk, Hv, K, V, *codes, *strides, 0, 0, qk_norm, eps, scale)
+    desc = DeltaDesc(B, L, Hk, Hv, K, V, *strides, 0, 0, *codes, 1 if qk_norm else 0, eps, scale)
+    ref, so = ctypes.byref(desc), lib()
     with _own_stream(stream):
-        o = torch.empty(tuple(v.shape), dtype=out_dtype, device=dev) if want_o else None
+        o = torch.empty(v.shape, dtype=out_dtype, device=dev) if want_o else None
         if want_hT and hT is None:
             hT = torch.empty((B, Hv, K, V), dtype=state_dtype, device=dev)
-        nbytes = delta_workspace_bytes(desc, starts is not None)
+        nbytes = so.precog_delta_workspace_bytes(ref, 0 if starts is None else 1)
         ws = torch.empty(nbytes, dtype=torch.uint8, device=dev) if nbytes else None
-    delta_encode(desc, q, k, v, g, beta, starts, h0, h0.shape[0] if h0 is not None else 0, h0_idx,
-                 o, hT, ws, nbytes, stream)
+    _check("precog_delta_encode", so.precog_delta_encode(
+        ref, _at(q), k.data_ptr(), v.data_ptr(), _at(g), _at(beta), _at(starts), _at(h0),
+        0 if h0 is None else h0.shape[0], _at(h0_idx), _at(o), _at(hT), _at(ws), nbytes,
+        _handle(stream, dev)))
     return o, hT
 
 
@@ -759,10 +770,12 @@ def delta_step(q, k, v, g, beta, states, slots, *, qk_norm=False, eps=1e-6, scal
     n = k.shape[0]
     _same("states", states, states.dtype, (states.shape[0], Hv, K, V), dev)
     _same("slots", slots, torch.int32, (n,), dev)
-    desc = delta_desc(n, 1, Hk, Hv, K, V, *codes, *strides, 0, 0, qk_norm, eps, scale)
+    desc = DeltaDesc(n, 1, Hk, Hv, K, V, *strides, 0, 0, *codes, 1 if qk_norm else 0, eps, scale)
     with _own_stream(stream):
         o = torch.empty((n, Hv, V), dtype=out_dtype, device=dev) if want_o else None
-    delta_step_raw(desc, q, k, v, g, beta, states, states.shape[0], slots, o, stream)
+    _check("precog_delta_step", lib().precog_delta_step(
+        ctypes.byref(desc), _at(q), k.data_ptr(), v.data_ptr(), _at(g), _at(beta),
+        states.data_ptr(), states.shape[0], slots.data_ptr(), _at(o), _handle(stream, dev)))
     return o
 
 
@@ -803,13 +816,15 @@ def conv(x, w, bias=None, tail0=None, *, starts=None, tail_idx=None, silu=True, 
         _same("tail0", tail0, x.dtype, (rows, W - 1, D), dev)
     if tailT is not None:
         _same("tailT", tailT, x.dtype, (B, W - 1, D), dev)
-    desc = conv_desc(B, L, D, W, *codes, stride, silu)
+    desc = ConvDesc(B, L, D, W, stride, *codes, 1 if silu else 0)
     with _own_stream(stream):
-        y = torch.empty(tuple(x.shape), dtype=out_dtype, device=dev) if want_y else None
+        y = torch.empty(x.shape, dtype=out_dtype, device=dev) if want_y else None
         if want_tail and tailT is None:
             tailT = torch.empty((B, max(W - 1, 0), D), dtype=x.dtype, device=dev)
-    conv_encode(desc, x, w, bias, starts, tail0, tail0.shape[0] if tail0 is not None else 0,
-                tail_idx, y, tailT, stream)
+    _check("precog_conv_encode", lib().precog_conv_encode(
+        ctypes.byref(desc), x.data_ptr(), w.data_ptr(), _at(bias), _at(starts), _at(tail0),
+        0 if tail0 is None else tail0.shape[0], _at(tail_idx), _at(y), _at(tailT),
+        _handle(stream, dev)))
     return y, tailT
 
 
@@ -822,10 +837,12 @@ def conv_step(x, w, bias, tails, slots, *, silu=True, out_dtype=None, stream=Non
     n = x.shape[0]
     _same("tails", tails, x.dtype, (tails.shape[0], W - 1, D), dev)
     _same("slots", slots, torch.int32, (n,), dev)
-    desc = conv_desc(n, 1, D, W, *codes, stride, silu)
+    desc = ConvDesc(n, 1, D, W, stride, *codes, 1 if silu else 0)
     with _own_stream(stream):
         y = torch.empty((n, D), dtype=out_dtype, device=dev)
-    conv_step_raw(desc, x, w, bias, tails, tails.shape[0], slots, y, stream)
+    _check("precog_conv_step", lib().precog_conv_step(
+        ctypes.byref(desc), x.data_ptr(), w.data_ptr(), _at(bias), tails.data_ptr(),
+        tails.shape[0], slots.data_ptr(), y.data_ptr(), _handle(stream, dev)))
     return y
 
 
@@ -848,13 +865,15 @@ def score_tokens(logits, token=None, top=0, *, want_entropy=True, stream=None):
         raise ValueError("top must be 0..64, not %d" % top)
     if token is not None:
         _same("token", token, torch.int32, (T,), dev)
-    nbytes = score_workspace_bytes(T, V, top)
+    L = lib()
+    nbytes = L.precog_score_workspace_bytes(T, V, top)
     with _own_stream(stream):
         logprob = torch.empty(T, dtype=torch.float32, device=dev) if token is not None else None
         entropy = torch.empty(T, dtype=torch.float32, device=dev) if want_entropy else None
         top_id = torch.empty((T, top), dtype=torch.int32, device=dev) if top else None
         top_logprob = torch.empty((T, top), dtype=torch.float32, device=dev) if top else None
         ws = torch.empty(nbytes, dtype=torch.uint8, device=dev) if nbytes else None
-    score_tokens_raw(logits, code, T, V, stride, token, top, logprob, entropy, top_id, top_logprob,
-                     ws, nbytes, stream)
+    _check("precog_score_tokens", L.precog_score_tokens(
+        logits.data_ptr(), code, T, V, stride, _at(token), top, _at(logprob), _at(entropy),
+        _at(top_id), _at(top_logprob), _at(ws), nbytes, _handle(stream, dev)))
     return logprob, entropy, top_id, top_logprob
