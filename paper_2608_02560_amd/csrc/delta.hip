@@ -38,7 +38,7 @@
 // known before they are.  Products of two low halves are left out (2^-22).  What
 // only enters a bf16 o (Q S, Q K^T U) takes the high halves alone: 2^-11 against
 // the 2^-8 of o.  Errors against 64 bits over 40,001 tokens: states 2.2e-7, as a
-// plain evaluation in 32 bits; two bf16 halves would leave 3e-6.
+// plain evaluation in 32 bits (two bf16 halves: 16 bits, some 3e-6 by that).
 //
 // What bounds it: vector instructions (65 % of the issue slots, beside 25 % for
 // the matrix ones, at 32 sequences of 3,000 tokens and 16 heads of 128 x 128:
