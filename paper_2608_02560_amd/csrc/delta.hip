@@ -35,10 +35,11 @@
 // inputs as two halves of 11 bits), and S, X, U and T as two halves (22 bits)
 // under a power of two of their own, a column's (T: a block's): X and T have
 // their largest at 2^14, S and U are held below 2^16 and 2^8 by bounds that are
-// known before they are.  Products of two low halves are left out (2^-22).  What
-// only enters a bf16 o (Q S, Q K^T U) takes the high halves alone: 2^-11 against
-// the 2^-8 of o.  Errors against 64 bits over 40,001 tokens: states 2.2e-7, as a
-// plain evaluation in 32 bits (two bf16 halves: 16 bits, some 3e-6 by that).
+// known before they are.  Products of two low halves are left out (2^-22).  A
+// bf16 o is computed as an fp32 one and rounded at the end: its two terms may
+// cancel, as they do where a value is replaced.  Errors against 64 bits over
+// 40,001 tokens: states 2.2e-7, as a plain evaluation in 32 bits (two bf16
+// halves: 16 bits, some 3e-6 by that).
 //
 // What bounds it: vector instructions (65 % of the issue slots, beside 25 % for
 // the matrix ones, at 32 sequences of 3,000 tokens and 16 heads of 128 x 128:
@@ -87,6 +88,13 @@ struct Factors {
 // What a call computes beside the states.
 constexpr int kNoOutput = 0, kOut16 = 1, kOut32 = 2;
 
+// A lower triangle of 32 x 32 numbers as two halves of operands: the rows of the
+// first token tile, whose depths 4 q + j are its own tokens, and of the second.
+struct Lower {
+  half4 first[2][64];
+  half8 second[2][64];
+};
+
 // A block's operands in LDS, in 1 KB fragments of one matrix instruction.
 template <int KP, bool IN32, int OUT>
 struct Buffer {
@@ -95,8 +103,8 @@ struct Buffer {
   half8 k[kHalves][2][kSteps][64];    // token tile, depth step
   half8 q[OUT ? kHalves : 0][2][kSteps][64];
   half8 kt[kHalves][KP / 16][64];     // state row tile; depth: the block's tokens
-  half8 t[2][2][64];                  // half, token tile
-  half8 p[OUT][2][64];                // half, token tile
+  Lower t;
+  Lower p[OUT ? 1 : 0];
   Factors f;
 };
 
@@ -109,15 +117,21 @@ struct Scratch {
   float beta[kBlockTokens];
 };
 
-// A and its inverse, 32 x 32 floats, take the place of T's operands until these
-// are made.  Groups of four columns are permuted within a row, so that 16 lanes
-// that read a column of groups meet different banks.
-__device__ __forceinline__ int a_at(int row, int col) { return 32 * row + 4 * (col / 4 ^ row % 8) + col % 4; }
+// A and its inverse take the place of T's operands until these are made: three
+// tiles of 16 x 16 floats, (0, 0), (1, 0) and (1, 1).  Groups of four columns are
+// permuted within a row, so that 16 lanes that read a column of groups meet
+// different banks, and neighbouring rows of the last tile change places, so that
+// a row of it and the same one of the first do.
+__device__ __forceinline__ int a_at(int row, int col) {
+  const int tile = row / 16 + col / 16, r = row % 16, c = col % 16;
+  return 256 * tile + 16 * (r ^ (tile == 2)) + 4 * (c / 4 ^ r / 4) + c % 4;
+}
+static_assert(sizeof(Lower) == 3 * 256 * sizeof(float), "A's tiles");
 
 template <int KP, bool IN32, int OUT>
 struct Shared {
   // as many as fit into the 160 KB of a CU, up to five
-  static constexpr int kBuffers = IN32 ? (KP == 128 ? 2 : 4) : KP == 128 && OUT == kOut32 ? 4 : 5;
+  static constexpr int kBuffers = IN32 ? (KP == 128 ? 2 : 4) : 5;
   static constexpr int kPrepare = kBuffers - 1;   // prepare waves: each works on a buffer of its own
   Buffer<KP, IN32, OUT> buf[kBuffers];
   Scratch scratch[kPrepare];
@@ -127,6 +141,9 @@ struct Shared {
 
 __device__ __forceinline__ float4v mfma(half8 a, half8 b, float4v c) {
   return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0);
+}
+__device__ __forceinline__ float4v mfma(half4 a, half4 b, float4v c) {
+  return __builtin_amdgcn_mfma_f32_16x16x16f16(a, b, c, 0, 0, 0);
 }
 __device__ __forceinline__ float4v mfma(float a, float b, float4v c) {
   return __builtin_amdgcn_mfma_f32_16x16x4f32(a, b, c, 0, 0, 0);
@@ -179,7 +196,7 @@ __device__ __forceinline__ float less_half(float x, half2 h) {
   return d;
 }
 
-// Eight fp32 values as halves of 11 bits each, or as the high ones alone.
+// Eight fp32 values as halves of 11 bits each, or four.
 __device__ __forceinline__ void split(const float4v& a, const float4v& b, half8& hi, half8& lo) {
   half2 h[4], l[4];
 #pragma unroll
@@ -191,11 +208,15 @@ __device__ __forceinline__ void split(const float4v& a, const float4v& b, half8&
   hi = half8{h[0][0], h[0][1], h[1][0], h[1][1], h[2][0], h[2][1], h[3][0], h[3][1]};
   lo = half8{l[0][0], l[0][1], l[1][0], l[1][1], l[2][0], l[2][1], l[3][0], l[3][1]};
 }
-__device__ __forceinline__ half8 high(const float4v& a, const float4v& b) {
+__device__ __forceinline__ void split(const float4v& a, half4& hi, half4& lo) {
   const half2 h0 = to_half2(a[0], a[1]), h1 = to_half2(a[2], a[3]);
-  const half2 h2 = to_half2(b[0], b[1]), h3 = to_half2(b[2], b[3]);
-  return half8{h0[0], h0[1], h1[0], h1[1], h2[0], h2[1], h3[0], h3[1]};
+  const half2 l0 = to_half2(less_half<0>(a[0], h0), less_half<1>(a[1], h0));
+  const half2 l1 = to_half2(less_half<0>(a[2], h1), less_half<1>(a[3], h1));
+  hi = half4{h0[0], h0[1], h1[0], h1[1]};
+  lo = half4{l0[0], l0[1], l1[0], l1[1]};
 }
+// The depths of the first token tile.
+__device__ __forceinline__ half4 first_tile(const half8& v) { return __builtin_shufflevector(v, v, 0, 1, 2, 3); }
 
 __device__ __forceinline__ int exponent(float v) { return static_cast<int>(__float_as_uint(v) >> 23 & 255); }
 
@@ -478,14 +499,8 @@ __device__ __forceinline__ void prepare_block(const DeltaParams& p, Inputs<KP, O
     *reinterpret_cast<float4v*>(&A[a_at(row, cols)]) = a;
   }
   if constexpr (outputs) {
-    const float4v none = {};
-#pragma unroll
-    for (int t = 0; t < 2; ++t) {
-      half8 hi, lo;
-      split(pm[t], t ? pm[2] : none, hi, lo);
-      buf.p[0][t][lane] = hi;
-      if (OUT == kOut32) buf.p[OUT - 1][t][lane] = lo;
-    }
+    split(pm[0], buf.p[0].first[0][lane], buf.p[0].first[1][lane]);
+    split(pm[1], pm[2], buf.p[0].second[0][lane], buf.p[0].second[1][lane]);
   }
   wave_fence();
 
@@ -535,7 +550,6 @@ __device__ __forceinline__ void prepare_block(const DeltaParams& p, Inputs<KP, O
   {
     const float4v beta0 = *reinterpret_cast<const float4v*>(&s.beta[4 * q]);
     const float4v beta1 = *reinterpret_cast<const float4v*>(&s.beta[16 + 4 * q]);
-    const float4v none = {};
     const float4v t11 = *reinterpret_cast<const float4v*>(&A[a_at(m, 4 * q)]) * beta0;
     const float4v t21 = *reinterpret_cast<const float4v*>(&A[a_at(16 + m, 4 * q)]) * beta0;
     const float4v tt2 = t22 * beta1;
@@ -544,14 +558,9 @@ __device__ __forceinline__ void prepare_block(const DeltaParams& p, Inputs<KP, O
     for (int r = 0; r < 4; ++r) most = max_abs(max_abs(max_abs(most, t11[r]), t21[r]), tt2[r]);
     const float t_most = wave_max(most);
     const Scale sc = scale_of(t_most);
-    half8 hi, lo;
     wave_fence();  // A has been read
-    split(t11 * sc.up, none, hi, lo);
-    buf.t[0][0][lane] = hi;
-    buf.t[1][0][lane] = lo;
-    split(t21 * sc.up, tt2 * sc.up, hi, lo);
-    buf.t[0][1][lane] = hi;
-    buf.t[1][1][lane] = lo;
+    split(t11 * sc.up, buf.t.first[0][lane], buf.t.first[1][lane]);
+    split(t21 * sc.up, tt2 * sc.up, buf.t.second[0][lane], buf.t.second[1][lane]);
     const float fo = p.scale * rq;
     const float eb = __builtin_amdgcn_exp2f(static_cast<float>(b2));
     const float fu = rk * __builtin_amdgcn_exp2f(static_cast<float>(readlane_d(b2, kBlockTokens - 1) - b2));
@@ -608,6 +617,19 @@ __device__ __forceinline__ void store_cols(__amdgpu_buffer_rsrc_t r, uint32_t of
       __builtin_amdgcn_raw_buffer_store_b32(
           narrow<T>(v[0]).bits | static_cast<uint32_t>(narrow<T>(v[1]).bits) << 16, r, off, 0, 0);
   }
+}
+
+// A lower triangle times 32 tokens of 16 columns, which are two halves.
+__device__ __forceinline__ void by_lower(const Lower& a, int lane, const half8& hi, const half8& lo, float4v& top,
+                                         float4v& bottom) {
+  const half4 a_hi = a.first[0][lane], a_lo = a.first[1][lane];
+  const half8 b_hi = a.second[0][lane], b_lo = a.second[1][lane];
+  top = mfma(a_hi, first_tile(hi), top);
+  bottom = mfma(b_hi, hi, bottom);
+  top = mfma(a_hi, first_tile(lo), top);
+  bottom = mfma(b_hi, lo, bottom);
+  top = mfma(a_lo, first_tile(hi), top);
+  bottom = mfma(b_lo, hi, bottom);
 }
 
 // The states of a wave's columns: row r of tile t is the state row 32 (t / 2) +
@@ -842,9 +864,9 @@ __global__ void __launch_bounds__(64 * (kChainMax + Shared<KP, IN32, OUT>::kPrep
 #pragma unroll
           for (int n = 0; n < NV; ++n) {
             qs[t][n] = mfma(qf, s_hi[n][st], qs[t][n]);
-            if (OUT == kOut32) qs[t][n] = mfma(qf, s_lo[n][st], qs[t][n]);
+            qs[t][n] = mfma(qf, s_lo[n][st], qs[t][n]);
           }
-          if (IN32 && OUT == kOut32) {
+          if (IN32) {
             const half8 ql = buf.q[kLow][t][st][at];
 #pragma unroll
             for (int n = 0; n < NV; ++n) qs[t][n] = mfma(ql, s_hi[n][st], qs[t][n]);
@@ -881,15 +903,7 @@ __global__ void __launch_bounds__(64 * (kChainMax + Shared<KP, IN32, OUT>::kPrep
         split(x[0][n] * sc.up, x[1][n] * sc.up, x_hi[n], x_lo[n]);
       }
 #pragma unroll
-      for (int t = 0; t < 2; ++t) {
-        const half8 t_hi = buf.t[0][t][lane], t_lo = buf.t[1][t][lane];
-#pragma unroll
-        for (int n = 0; n < NV; ++n) {
-          u[t][n] = mfma(t_hi, x_hi[n], u[t][n]);
-          u[t][n] = mfma(t_hi, x_lo[n], u[t][n]);
-          u[t][n] = mfma(t_lo, x_hi[n], u[t][n]);
-        }
-      }
+      for (int n = 0; n < NV; ++n) by_lower(buf.t, lane, x_hi[n], x_lo[n], u[0][n], u[1][n]);
     }
     // U / sigma' as two operands: |k| U for Q K^T, e^{b_end - b} |k| U for K^T
     half8 u_hi[NV], u_lo[NV], w_hi[NV], w_lo[NV];
@@ -917,10 +931,7 @@ __global__ void __launch_bounds__(64 * (kChainMax + Shared<KP, IN32, OUT>::kPrep
         u[0][n] *= unit;
         u[1][n] *= unit;
         split(u[0][n] * fu[0], u[1][n] * fu[1], u_hi[n], u_lo[n]);
-        if (OUT == kOut32)
-          split(u[0][n] * fr[0], u[1][n] * fr[1], w_hi[n], w_lo[n]);
-        else if (OUT == kOut16)
-          w_hi[n] = high(u[0][n] * fr[0], u[1][n] * fr[1]);
+        if (OUT) split(u[0][n] * fr[0], u[1][n] * fr[1], w_hi[n], w_lo[n]);
       }
     }
 #pragma unroll
@@ -938,18 +949,11 @@ __global__ void __launch_bounds__(64 * (kChainMax + Shared<KP, IN32, OUT>::kPrep
       const __amdgpu_buffer_rsrc_t ro =
           make_rsrc(o_at, (rows_of(c) - 1) * o_step + p.V * static_cast<uint32_t>(sizeof(TOut)));
       o_at += static_cast<int64_t>(kBlockTokens) * p.Hv * p.V;
+      float4v pu[2][NV] = {};
+#pragma unroll
+      for (int n = 0; n < NV; ++n) by_lower(buf.p[0], lane, w_hi[n], w_lo[n], pu[0][n], pu[1][n]);
 #pragma unroll
       for (int t = 0; t < 2; ++t) {
-        const half8 pf = buf.p[0][t][lane];
-        float4v pu[NV] = {};
-#pragma unroll
-        for (int n = 0; n < NV; ++n) {
-          pu[n] = mfma(pf, w_hi[n], pu[n]);
-          if (OUT == kOut32) {
-            pu[n] = mfma(pf, w_lo[n], pu[n]);
-            pu[n] = mfma(buf.p[OUT - 1][t][lane], w_hi[n], pu[n]);
-          }
-        }
         const float4v fq = *reinterpret_cast<const float4v*>(&buf.f.q[16 * t + 4 * q]);
         const float4v fo = *reinterpret_cast<const float4v*>(&buf.f.o[16 * t + 4 * q]);
 #pragma unroll
@@ -957,7 +961,7 @@ __global__ void __launch_bounds__(64 * (kChainMax + Shared<KP, IN32, OUT>::kPrep
           float v[NV];
 #pragma unroll
           for (int n = 0; n < NV; ++n)
-            v[n] = fq[r] * (sigma[n] * qs[t][n][r]) + fo[r] * (next[n] * pu[n][r]);
+            v[n] = fq[r] * (sigma[n] * qs[t][n][r]) + fo[r] * (next[n] * pu[t][n][r]);
           store_cols<TOut, NV>(ro, o_off + (16 * t + r) * o_step, v);
         }
       }

@@ -1,0 +1,55 @@
+"""The gated delta rule on the GPU where numbers of very different size meet in
+one block of tokens: every o and every column of the states is held to what the
+head itself had when the error was made (layer_ranges.py), and the small numbers
+are checked as closely as the large ones."""
+import numpy as np
+import pytest
+import torch
+
+from layer_ranges import near, sizes
+from layer_testutil import delta_bar, delta_inputs, delta_oracle, on_gpu, starts_of
+from paper_2608_02560_amd import precog as P
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda"
+IO = [torch.bfloat16, torch.float32]
+
+
+def _run(d, lens, h0=None, norm=True, out=torch.float32, bar_tokens=None, **kw):
+    """o and the states against the oracle; delta_bar of the longest sequence,
+    counted from the sizes (a state's element: from its column's norm over
+    sqrt(K))."""
+    c = on_gpu(d)
+    K = d["k"].shape[-1]
+    o, hT = P.delta(c["q"], c["k"], c["v"], c["g"], c["beta"], None if h0 is None else h0.to(DEV),
+                    starts=starts_of(lens).to(DEV), qk_norm=norm, out_dtype=out, **kw)
+    ro, rS = delta_oracle(d, lens, h0, qk_norm=norm)
+    so, sS = sizes(d, lens, h0, norm)
+    bar = delta_bar(bar_tokens or max(lens))
+    near(o, ro, so, bar, "o")
+    near(hT, rS, np.broadcast_to(sS[:, :, None] * K ** -0.5, rS.shape), bar, "hT")
+
+
+@pytest.mark.parametrize("dtype", IO)
+@pytest.mark.parametrize("ratio", [1.0, 0.1, 0.01])
+def test_bf16_outputs_where_values_are_replaced(dtype, ratio):
+    """beta = 1 and the same keys again with smaller values: o is the difference
+    of the old value's two terms, and is rounded to its type only at the end."""
+    d = delta_inputs(96, 1, 2, 64, 64, 101, dtype, sliced=False)
+    d["k"][32:64] = d["k"][:32]
+    d["k"][64:] = d["k"][:32]
+    d["q"][:] = d["k"]
+    d["v"][32:64] = (d["v"][32:64].float() * ratio).to(dtype)
+    d["v"][64:] = (d["v"][64:].float() * ratio * ratio).to(dtype)
+    d["beta"][:] = 1.0
+    d["g"][:] = 0.0
+    _run(d, [96], out=torch.bfloat16)
+
+
+def test_bf16_outputs_are_the_rounded_fp32_ones():
+    """The storage type of o changes nothing but its last rounding."""
+    d = on_gpu(delta_inputs(200, 2, 4, 128, 128, 102))
+    s = starts_of([77, 123]).to(DEV)
+    a, sa = P.delta(d["q"], d["k"], d["v"], d["g"], d["beta"], starts=s, qk_norm=True)
+    b, sb = P.delta(d["q"], d["k"], d["v"], d["g"], d["beta"], starts=s, qk_norm=True, out_dtype=torch.bfloat16)
+    assert torch.equal(a.bfloat16(), b) and torch.equal(sa, sb)
