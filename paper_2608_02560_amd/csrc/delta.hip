@@ -4,10 +4,15 @@
 // exp(b_i - b_j) for i >= j, S the state before the block and u_i the values
 // that the tokens write:
 //
-//   A_ij = beta_i G_ij k_i.k_j  (i > j),   T = (I + A)^-1 diag(beta)
-//   X = V - diag(e^b) K S,   U = T X
+//   A_ij = beta_i G_ij k_i.k_j  (i > j),   T = (I + A)^-1
+//   X = diag(beta) (V - diag(e^b) K S),   U = T X
 //   O = scale (diag(e^b) Q S + (G . Q K^T) U)
 //   S <- e^{b_end} S + K^T diag(e^{b_end - b}) U
+//
+// (the gate with the values, not with T: a closed one keeps a value out of X's
+// scale, however large) and, for keys of any length |k|, u' = |k| u in place of u:
+// with k^ = k / |k|, A_ij = beta_i |k_i|^2 G_ij k^_i.k^_j and X = diag(beta |k|) V -
+// diag(beta |k|^2 e^b) K^ S.
 //
 // so a block is a handful of small matrix products, and only those with S
 // depend on the block before.  One workgroup owns one head of one sequence (or
@@ -74,14 +79,14 @@ typedef uint32_t uint4v __attribute__((ext_vector_type(4)));
 
 // Row factors of a block's tokens, and what belongs to the block.
 struct Factors {
-  float x[kBlockTokens];   // e^b |k| of X's subtrahend
-  float r[kBlockTokens];   // |k| of a row of U before Q K^T
-  float u[kBlockTokens];   // e^{b_end - b} |k| of a row of U before K^T
+  float v[kBlockTokens];   // beta |k| of V
+  float x[kBlockTokens];   // beta |k|^2 e^b of X's subtrahend
+  float u[kBlockTokens];   // e^{b_end - b} of a row of U before K^T
   float q[kBlockTokens];   // scale |q| e^b of Q S
   float o[kBlockTokens];   // scale |q| of Q K^T U
   float decay;             // e^{b_end}
   float t;                 // power of two that T's operand lacks
-  float most;              // bound of r U and u U for |X| <= 1
+  float most;              // bound of U and u U for |X| <= 1
   float pad;
 };
 
@@ -114,7 +119,7 @@ struct Scratch {
   float b[kBlockTokens], b_low[kBlockTokens];
   float rk[kBlockTokens];
   float rq[kBlockTokens];
-  float beta[kBlockTokens];
+  float beta[kBlockTokens];   // beta |k|^2
 };
 
 // A and its inverse take the place of T's operands until these are made: three
@@ -427,16 +432,18 @@ __device__ __forceinline__ void prepare_block(const DeltaParams& p, Inputs<KP, O
   make_operand<KP, IN32, true, TIn>(in.k, buf.k, buf.kt, s.rk);
   if constexpr (outputs) make_operand<KP, IN32, false, TIn>(in.q, buf.q, buf.kt, s.rq);
   wave_fence();
-  // lane l has token l % 32 (a token behind the last one has no key and no query)
+  // lane l has token l % 32 (a token behind the last one has no key and no query;
+  // a key of zeros has no length either, so its value does not reach X)
   const bool live = lane % kBlockTokens < in.rows;
-  const float rk = live ? row_factor(s.rk[lane % kBlockTokens], p.norm, p.eps) : 0.f;
+  const float sq = s.rk[lane % kBlockTokens];
+  const float rk = live && sq != 0.f ? row_factor(sq, p.norm, p.eps) : 0.f;
   const float rq = live && outputs ? row_factor(s.rq[lane % kBlockTokens], p.norm, p.eps) : 0.f;
   const double b2 = b * 1.4426950408889634;
+  const float gate = in.beta * rk;
   if (lane < kBlockTokens) {
     s.b[lane] = static_cast<float>(b2);
     s.b_low[lane] = static_cast<float>(b2 - static_cast<double>(s.b[lane]));
-    s.rk[lane] = rk;
-    s.beta[lane] = in.beta;
+    s.beta[lane] = in.beta * rk * rk;
   }
   next();
   wave_fence();
@@ -483,16 +490,15 @@ __device__ __forceinline__ void prepare_block(const DeltaParams& p, Inputs<KP, O
 #pragma unroll
   for (int i = 0; i < 3; ++i) {
     const int ti = i > 0, tj = i / 2, row = 16 * ti + m, cols = 16 * tj + 4 * q;
-    const float bi = s.b[row], bi_low = s.b_low[row], ri = s.rk[row] * s.beta[row];
+    const float bi = s.b[row], bi_low = s.b_low[row], ri = s.beta[row];
     const float4v bj = *reinterpret_cast<const float4v*>(&s.b[cols]);
     const float4v bj_low = *reinterpret_cast<const float4v*>(&s.b_low[cols]);
-    const float4v rj = *reinterpret_cast<const float4v*>(&s.rk[cols]);
     float4v a;
 #pragma unroll
     for (int r = 0; r < 4; ++r) {
       const float d = (bi - bj[r]) + (bi_low - bj_low[r]);
       const float decay = __builtin_amdgcn_exp2f(ti > tj || row >= cols + r ? d : -__builtin_inff());
-      const float v = ri * rj[r] * (decay * kk[i][r]);
+      const float v = ri * (decay * kk[i][r]);
       a[r] = ti > tj || row > cols + r ? v : 0.f;
       pm[i][r] = decay * qk[i][r];
     }
@@ -548,26 +554,23 @@ __device__ __forceinline__ void prepare_block(const DeltaParams& p, Inputs<KP, O
   for (int r = 0; r < 4; ++r) A[a_at(16 + 4 * q + r, m)] = -z[r];
   wave_fence();
   {
-    const float4v beta0 = *reinterpret_cast<const float4v*>(&s.beta[4 * q]);
-    const float4v beta1 = *reinterpret_cast<const float4v*>(&s.beta[16 + 4 * q]);
-    const float4v t11 = *reinterpret_cast<const float4v*>(&A[a_at(m, 4 * q)]) * beta0;
-    const float4v t21 = *reinterpret_cast<const float4v*>(&A[a_at(16 + m, 4 * q)]) * beta0;
-    const float4v tt2 = t22 * beta1;
+    const float4v t11 = *reinterpret_cast<const float4v*>(&A[a_at(m, 4 * q)]);
+    const float4v t21 = *reinterpret_cast<const float4v*>(&A[a_at(16 + m, 4 * q)]);
     float most = 0.f;
 #pragma unroll
-    for (int r = 0; r < 4; ++r) most = max_abs(max_abs(max_abs(most, t11[r]), t21[r]), tt2[r]);
+    for (int r = 0; r < 4; ++r) most = max_abs(max_abs(max_abs(most, t11[r]), t21[r]), t22[r]);
     const float t_most = wave_max(most);
     const Scale sc = scale_of(t_most);
     wave_fence();  // A has been read
     split(t11 * sc.up, buf.t.first[0][lane], buf.t.first[1][lane]);
-    split(t21 * sc.up, tt2 * sc.up, buf.t.second[0][lane], buf.t.second[1][lane]);
+    split(t21 * sc.up, t22 * sc.up, buf.t.second[0][lane], buf.t.second[1][lane]);
     const float fo = p.scale * rq;
     const float eb = __builtin_amdgcn_exp2f(static_cast<float>(b2));
-    const float fu = rk * __builtin_amdgcn_exp2f(static_cast<float>(readlane_d(b2, kBlockTokens - 1) - b2));
-    const float largest = wave_max(fmaxf(rk, fu));
+    const float fu = __builtin_amdgcn_exp2f(static_cast<float>(readlane_d(b2, kBlockTokens - 1) - b2));
+    const float largest = wave_max(fmaxf(1.f, fu));
     if (lane < kBlockTokens) {
-      buf.f.x[lane] = rk * eb;
-      buf.f.r[lane] = rk;
+      buf.f.v[lane] = gate;
+      buf.f.x[lane] = gate * rk * eb;
       buf.f.u[lane] = fu;
       buf.f.q[lane] = fo * eb;
       buf.f.o[lane] = fo;
@@ -882,10 +885,11 @@ __global__ void __launch_bounds__(64 * (kChainMax + Shared<KP, IN32, OUT>::kPrep
 #pragma unroll
       for (int t = 0; t < 2; ++t) {
         const float4v fx = *reinterpret_cast<const float4v*>(&buf.f.x[16 * t + 4 * q]);
+        const float4v fv = *reinterpret_cast<const float4v*>(&buf.f.v[16 * t + 4 * q]);
 #pragma unroll
         for (int n = 0; n < NV; ++n)
 #pragma unroll
-          for (int r = 0; r < 4; ++r) x[t][n][r] = col_value<TIn>(raw[t][r], n) - fx[r] * sigma[n] * ks[t][n][r];
+          for (int r = 0; r < 4; ++r) x[t][n][r] = fv[r] * col_value<TIn>(raw[t][r], n) - fx[r] * sigma[n] * ks[t][n][r];
       }
       if (c + 1 < blocks) fetch(c + 1);
       half8 x_hi[NV], x_lo[NV];
@@ -905,16 +909,13 @@ __global__ void __launch_bounds__(64 * (kChainMax + Shared<KP, IN32, OUT>::kPrep
 #pragma unroll
       for (int n = 0; n < NV; ++n) by_lower(buf.t, lane, x_hi[n], x_lo[n], u[0][n], u[1][n]);
     }
-    // U / sigma' as two operands: |k| U for Q K^T, e^{b_end - b} |k| U for K^T
+    // U / sigma' as two operands: U for Q K^T, e^{b_end - b} U for K^T
     half8 u_hi[NV], u_lo[NV], w_hi[NV], w_lo[NV];
     float next[NV], keep[NV];  // sigma', and the factor of S~
     {
-      float4v fr[2], fu[2];
+      float4v fu[2];
 #pragma unroll
-      for (int t = 0; t < 2; ++t) {
-        fr[t] = *reinterpret_cast<const float4v*>(&buf.f.r[16 * t + 4 * q]);
-        fu[t] = *reinterpret_cast<const float4v*>(&buf.f.u[16 * t + 4 * q]);
-      }
+      for (int t = 0; t < 2; ++t) fu[t] = *reinterpret_cast<const float4v*>(&buf.f.u[16 * t + 4 * q]);
       const float decay = buf.f.decay;
 #pragma unroll
       for (int n = 0; n < NV; ++n) {
@@ -931,7 +932,7 @@ __global__ void __launch_bounds__(64 * (kChainMax + Shared<KP, IN32, OUT>::kPrep
         u[0][n] *= unit;
         u[1][n] *= unit;
         split(u[0][n] * fu[0], u[1][n] * fu[1], u_hi[n], u_lo[n]);
-        if (OUT) split(u[0][n] * fr[0], u[1][n] * fr[1], w_hi[n], w_lo[n]);
+        if (OUT) split(u[0][n], u[1][n], w_hi[n], w_lo[n]);
       }
     }
 #pragma unroll

@@ -53,3 +53,36 @@ def test_bf16_outputs_are_the_rounded_fp32_ones():
     a, sa = P.delta(d["q"], d["k"], d["v"], d["g"], d["beta"], starts=s, qk_norm=True)
     b, sb = P.delta(d["q"], d["k"], d["v"], d["g"], d["beta"], starts=s, qk_norm=True, out_dtype=torch.bfloat16)
     assert torch.equal(a.bfloat16(), b) and torch.equal(sa, sb)
+
+
+@pytest.mark.parametrize("dtype", IO)
+@pytest.mark.parametrize("size", [1e6, 1e30])
+def test_closed_gates_hide_large_values(dtype, size):
+    """beta = 0 keeps a value out, however large (rows of padding)."""
+    d = delta_inputs(100, 1, 2, 64, 64, 121, dtype, sliced=False)
+    for t in (3, 17, 40, 41, 99):
+        d["v"][t] = (d["v"][t].float() * size).to(dtype)
+        d["beta"][t] = 0.0
+    _run(d, [100])
+
+
+@pytest.mark.parametrize("dtype", IO)
+@pytest.mark.parametrize("size", [1e6, 1e20])
+def test_zero_keys_hide_large_values(dtype, size):
+    """A token without a key writes nothing, whatever its value and gate."""
+    d = delta_inputs(100, 1, 2, 64, 64, 122, dtype, sliced=False)
+    for t in (0, 20, 50, 99):
+        d["v"][t] = (d["v"][t].float() * size).to(dtype)
+        d["k"][t] = 0
+    _run(d, [100])
+
+
+@pytest.mark.parametrize("dtype", IO)
+def test_long_keys_without_values(dtype):
+    """Keys of very different length as they are given: the long ones write nothing."""
+    d = delta_inputs(96, 1, 2, 64, 64, 112, dtype, unit=True, sliced=False)
+    long = torch.arange(96) % 3 == 0
+    d["k"][~long] = (d["k"][~long].float() * 2.0 ** -20).to(dtype)
+    d["v"][long] = 0
+    d["beta"][long] = 0
+    _run(d, [96], norm=False)
