@@ -37,10 +37,10 @@
 // fp64, where the differences of two positions are taken).  A product's
 // operands are fp16: keys and queries under the power of two that brings the
 // row's norm to [1, 2) (exact for bf16 down to 2^-16 of it, good to 2^-25; fp32
-// inputs as two halves of 11 bits), and S, X, U and T as two halves (22 bits)
-// under a power of two of their own, a column's (T: a block's): X and T have
-// their largest at 2^14, S and U are held below 2^16 and 2^8 by bounds that are
-// known before they are.  Products of two low halves are left out (2^-22).  A
+// inputs as two halves of 11 bits; queries under 2^12 more, which leaves G . Q K^T
+// its 22 bits under decays down to e^-9), and S, X, U and T as two halves (22 bits)
+// under a power of two of their own, a column's (T: a block's): X, T and the U of
+// O have their largest at 2^14, S and its U are held below 2^16 and 2^8.  Products of two low halves are left out (2^-22).  A
 // bf16 o is computed as an fp32 one and rounded at the end: its two terms may
 // cancel, as they do where a value is replaced.  Errors against 64 bits over
 // 40,001 tokens: states 2.2e-7, as a plain evaluation in 32 bits (two bf16
@@ -67,6 +67,7 @@ namespace {
 
 constexpr int kBlockTokens = 32;
 constexpr int kChainMax = 4;     // chain waves of a workgroup
+constexpr float kQueryUp = 4096.f;  // power of two of queries above that of keys
 
 typedef _Float16 half8 __attribute__((ext_vector_type(8)));
 typedef _Float16 half4 __attribute__((ext_vector_type(4)));
@@ -86,8 +87,7 @@ struct Factors {
   float o[kBlockTokens];   // scale |q| of Q K^T U
   float decay;             // e^{b_end}
   float t;                 // power of two that T's operand lacks
-  float most;              // bound of U and u U for |X| <= 1
-  float pad;
+  float pad[2];
 };
 
 // What a call computes beside the states.
@@ -336,10 +336,11 @@ __device__ __forceinline__ float row_factor(float sq, int norm, float eps) {
   return norm ? down * __builtin_amdgcn_rsqf(sq + eps) : down;
 }
 
-// Rows as operands in LDS (and, for keys, transposed ones), and every token's
-// sum of squares.
+// Rows times `more` as operands in LDS (and, for keys, transposed ones), and every
+// token's sum of squares.
 template <int KP, bool IN32, bool TRANSPOSE, typename TIn, typename Frags, typename FragsT>
-__device__ __forceinline__ void make_operand(const Rows<KP, TIn>& rows, Frags& frags, FragsT& turned, float* squares) {
+__device__ __forceinline__ void make_operand(const Rows<KP, TIn>& rows, Frags& frags, FragsT& turned, float* squares,
+                                             float more) {
   using R = Rows<KP, TIn>;
   const int lane = fresh_lane(), c = lane % R::kLanes, row = lane / 16;
 #pragma unroll
@@ -348,7 +349,7 @@ __device__ __forceinline__ void make_operand(const Rows<KP, TIn>& rows, Frags& f
     float v[8];
     rows.values(i, v);
     const float sq = row_sum<KP>(rows.squares(i, v));
-    const float up = row_scale(sq).up;
+    const float up = row_scale(sq).up * more;
     if (c == 0) squares[4 * lp + row] = sq;
     uint32_t word[2][4];
 #pragma unroll
@@ -429,15 +430,15 @@ __device__ __forceinline__ void prepare_block(const DeltaParams& p, Inputs<KP, O
     const double up = __shfl_up(b, d, kBlockTokens);
     if (lane % kBlockTokens >= d) b += up;
   }
-  make_operand<KP, IN32, true, TIn>(in.k, buf.k, buf.kt, s.rk);
-  if constexpr (outputs) make_operand<KP, IN32, false, TIn>(in.q, buf.q, buf.kt, s.rq);
+  make_operand<KP, IN32, true, TIn>(in.k, buf.k, buf.kt, s.rk, 1.f);
+  if constexpr (outputs) make_operand<KP, IN32, false, TIn>(in.q, buf.q, buf.kt, s.rq, kQueryUp);
   wave_fence();
   // lane l has token l % 32 (a token behind the last one has no key and no query;
   // a key of zeros has no length either, so its value does not reach X)
   const bool live = lane % kBlockTokens < in.rows;
   const float sq = s.rk[lane % kBlockTokens];
   const float rk = live && sq != 0.f ? row_factor(sq, p.norm, p.eps) : 0.f;
-  const float rq = live && outputs ? row_factor(s.rq[lane % kBlockTokens], p.norm, p.eps) : 0.f;
+  const float rq = live && outputs ? row_factor(s.rq[lane % kBlockTokens], p.norm, p.eps) / kQueryUp : 0.f;
   const double b2 = b * 1.4426950408889634;
   const float gate = in.beta * rk;
   if (lane < kBlockTokens) {
@@ -567,7 +568,6 @@ __device__ __forceinline__ void prepare_block(const DeltaParams& p, Inputs<KP, O
     const float fo = p.scale * rq;
     const float eb = __builtin_amdgcn_exp2f(static_cast<float>(b2));
     const float fu = __builtin_amdgcn_exp2f(static_cast<float>(readlane_d(b2, kBlockTokens - 1) - b2));
-    const float largest = wave_max(fmaxf(1.f, fu));
     if (lane < kBlockTokens) {
       buf.f.v[lane] = gate;
       buf.f.x[lane] = gate * rk * eb;
@@ -577,7 +577,6 @@ __device__ __forceinline__ void prepare_block(const DeltaParams& p, Inputs<KP, O
       if (lane == kBlockTokens - 1) buf.f.decay = eb;
       if (lane == 0) {
         buf.f.t = sc.down;
-        buf.f.most = kBlockTokens * t_most * largest;
       }
     }
   }
@@ -802,11 +801,14 @@ __global__ void __launch_bounds__(64 * (kChainMax + Shared<KP, IN32, OUT>::kPrep
   // |S~| < 2^16: its halves are fp16 numbers as they are.  `bound` >= |S~|.
   // A block multiplies S~ by decay sigma / sigma' and adds K^T (U / sigma'),
   // where 32 keys' elements of at most 2 meet |U / sigma'| < 2^8: sigma' is
-  // chosen so that both terms stay below 2^14, from bounds that are known before
-  // U is (|U| <= 32 |T| |X|).  The halves' floor of 2^-24 leaves them 22 bits of
-  // the column's largest while that is above 2^-2; U's bound is some 2^7 above
-  // it, and that of S~, which can grow by 2^14 a block, is taken anew from S~
-  // every eighth block.
+  // chosen so that both terms stay below 2^14, from the largest element that U
+  // has under its decays to the block's end (what a block wrote and has forgotten
+  // by then sets no scale) and from S~'s bound.  The halves' floor of 2^-24 leaves
+  // them 22 bits of the column's largest while that is above 2^-2; the bound of
+  // S~, which can grow by 2^6 times U a block, is taken anew from S~ every eighth
+  // block.  (Bounds of U that are known before it is, 32 |T| |X|, would take 2 %
+  // of the time away and lost all of a state that a block's last tokens shrink by
+  // 2^24.)
   float sigma[NV], bound[NV];
   const auto largest = [&](int n) {
     float most = 0.f;
@@ -879,7 +881,7 @@ __global__ void __launch_bounds__(64 * (kChainMax + Shared<KP, IN32, OUT>::kPrep
     }
     // X, then U = T X without the powers of two of their operands
     float4v u[2][NV] = {};
-    float u_unit[NV], u_most[NV];
+    float u_unit[NV];
     {
       float4v x[2][NV];
 #pragma unroll
@@ -903,15 +905,15 @@ __global__ void __launch_bounds__(64 * (kChainMax + Shared<KP, IN32, OUT>::kPrep
         most = max_of_rows(most);
         const Scale sc = scale_of(most);
         u_unit[n] = sc.down * buf.f.t;
-        u_most[n] = most * buf.f.most;
         split(x[0][n] * sc.up, x[1][n] * sc.up, x_hi[n], x_lo[n]);
       }
 #pragma unroll
       for (int n = 0; n < NV; ++n) by_lower(buf.t, lane, x_hi[n], x_lo[n], u[0][n], u[1][n]);
     }
-    // U / sigma' as two operands: U for Q K^T, e^{b_end - b} U for K^T
+    // U / sigma' under its decays for K^T, and U under a power of two of its own
+    // for Q K^T
     half8 u_hi[NV], u_lo[NV], w_hi[NV], w_lo[NV];
-    float next[NV], keep[NV];  // sigma', and the factor of S~
+    float next[NV], keep[NV], w_unit[NV];  // sigma', the factor of S~, what U for Q K^T lacks
     {
       float4v fu[2];
 #pragma unroll
@@ -919,20 +921,35 @@ __global__ void __launch_bounds__(64 * (kChainMax + Shared<KP, IN32, OUT>::kPrep
       const float decay = buf.f.decay;
 #pragma unroll
       for (int n = 0; n < NV; ++n) {
-        // the last term bounds sigma / sigma' by 2^64 where S and U vanish
-        int e = exponent(u_most[n]) - 7;
-        e = max(e, exponent(bound[n] * sigma[n] * decay) - 13);
-        e = max(e, exponent(sigma[n]) - 64);
+        const float4v end[2] = {u[0][n] * fu[0], u[1][n] * fu[1]};
+        float most = 0.f, all = 0.f;
+#pragma unroll
+        for (int t = 0; t < 2; ++t)
+#pragma unroll
+          for (int r = 0; r < 4; ++r) {
+            most = max_abs(most, end[t][r]);
+            all = max_abs(all, u[t][n][r]);
+          }
+        most = max_of_rows(most) * u_unit[n];
+        // the last terms keep the factors of S~ and of U in fp32 where S or U vanish
+        const float left = sigma[n] * decay;
+        int e = exponent(most) - 7;
+        e = max(e, exponent(bound[n] * left) - 13);
+        e = max(e, exponent(left) - 64);
+        e = max(e, exponent(u_unit[n]) - 100);
         e = min(max(e, 2), 252);
         next[n] = __uint_as_float(static_cast<uint32_t>(e) << 23);
         const float up = __uint_as_float(static_cast<uint32_t>(254 - e) << 23);
-        keep[n] = sigma[n] * up * decay;
-        bound[n] = bound[n] * keep[n] + 64.f * (u_most[n] * up);
+        keep[n] = left * up;
+        bound[n] = bound[n] * keep[n] + 64.f * (most * up);
         const float unit = u_unit[n] * up;
-        u[0][n] *= unit;
-        u[1][n] *= unit;
-        split(u[0][n] * fu[0], u[1][n] * fu[1], u_hi[n], u_lo[n]);
-        if (OUT) split(u[0][n], u[1][n], w_hi[n], w_lo[n]);
+        split(end[0] * unit, end[1] * unit, u_hi[n], u_lo[n]);
+        if (OUT) {
+          const Scale sc = scale_of(max_of_rows(all) * u_unit[n]);
+          w_unit[n] = sc.down;
+          const float own = u_unit[n] * sc.up;
+          split(u[0][n] * own, u[1][n] * own, w_hi[n], w_lo[n]);
+        }
       }
     }
 #pragma unroll
@@ -962,7 +979,7 @@ __global__ void __launch_bounds__(64 * (kChainMax + Shared<KP, IN32, OUT>::kPrep
           float v[NV];
 #pragma unroll
           for (int n = 0; n < NV; ++n)
-            v[n] = fq[r] * (sigma[n] * qs[t][n][r]) + fo[r] * (next[n] * pu[t][n][r]);
+            v[n] = fq[r] * (sigma[n] * qs[t][n][r]) + fo[r] * (w_unit[n] * pu[t][n][r]);
           store_cols<TOut, NV>(ro, o_off + (16 * t + r) * o_step, v);
         }
       }

@@ -86,3 +86,30 @@ def test_long_keys_without_values(dtype):
     d["v"][long] = 0
     d["beta"][long] = 0
     _run(d, [96], norm=False)
+
+
+@pytest.mark.parametrize("dtype", IO)
+@pytest.mark.parametrize("g", [-4.0, -6.0, -8.0])
+@pytest.mark.parametrize("first", [0, 32])
+def test_blocks_that_end_in_decay(dtype, g, first):
+    """The last tokens of a block forget and write nothing: what is left is small
+    beside what the block wrote, and is all that the next block reads."""
+    n = first + 32
+    d = delta_inputs(n + 40, 1, 2, 64, 64, 111, dtype)
+    d["g"][n - 1] = g
+    d["beta"][n - 1:] = 0.0
+    d["g"][n:] = 0.0
+    _run(d, [n + 40])
+    _run({x: t[:n] for x, t in d.items()}, [n])
+
+
+@pytest.mark.parametrize("dtype", IO)
+@pytest.mark.parametrize("size", [1e3, 1e4])
+def test_large_values_before_a_reset(dtype, size):
+    """A large value and a token that forgets it in one block; the following
+    blocks' small numbers are as good as without it."""
+    d = delta_inputs(420, 1, 2, 64, 64, 113, dtype, sliced=False)
+    d["v"][5] = (d["v"][5].float() * size).to(dtype)
+    d["g"][20] = -np.inf
+    _run(d, [420], bar_tokens=100)
+    _run(d, [50, 370], bar_tokens=100)
