@@ -223,6 +223,12 @@ __device__ __forceinline__ void split(const float4v& a, half4& hi, half4& lo) {
 // The depths of the first token tile.
 __device__ __forceinline__ half4 first_tile(const half8& v) { return __builtin_shufflevector(v, v, 0, 1, 2, 3); }
 
+// 2^x.  The integer part by itself: in fp32 2^-90 would be good to 2^-18.
+__device__ __forceinline__ float exp2_of(double x) {
+  const double whole = rint(x);
+  return __builtin_ldexpf(__builtin_amdgcn_exp2f(static_cast<float>(x - whole)), static_cast<int>(whole));
+}
+
 __device__ __forceinline__ int exponent(float v) { return static_cast<int>(__float_as_uint(v) >> 23 & 255); }
 
 __device__ __forceinline__ int uniform(int v) { return __builtin_amdgcn_readfirstlane(v); }
@@ -566,8 +572,8 @@ __device__ __forceinline__ void prepare_block(const DeltaParams& p, Inputs<KP, O
     split(t11 * sc.up, buf.t.first[0][lane], buf.t.first[1][lane]);
     split(t21 * sc.up, t22 * sc.up, buf.t.second[0][lane], buf.t.second[1][lane]);
     const float fo = p.scale * rq;
-    const float eb = __builtin_amdgcn_exp2f(static_cast<float>(b2));
-    const float fu = __builtin_amdgcn_exp2f(static_cast<float>(readlane_d(b2, kBlockTokens - 1) - b2));
+    const float eb = exp2_of(b2);
+    const float fu = exp2_of(readlane_d(b2, kBlockTokens - 1) - b2);
     if (lane < kBlockTokens) {
       buf.f.v[lane] = gate;
       buf.f.x[lane] = gate * rk * eb;
@@ -931,19 +937,20 @@ __global__ void __launch_bounds__(64 * (kChainMax + Shared<KP, IN32, OUT>::kPrep
             all = max_abs(all, u[t][n][r]);
           }
         most = max_of_rows(most) * u_unit[n];
-        // the last terms keep the factors of S~ and of U in fp32 where S or U vanish
-        const float left = sigma[n] * decay;
+        // exponents of sigma' for U, for S~, and the least, where both vanish (the
+        // last one of all keeps U's factor in fp32)
+        const int unit = exponent(sigma[n]);
         int e = exponent(most) - 7;
-        e = max(e, exponent(bound[n] * left) - 13);
-        e = max(e, exponent(left) - 64);
+        e = max(e, exponent(bound[n] * decay) + unit - 127 - 13);
+        e = max(e, exponent(decay) + unit - 127 - 64);
         e = max(e, exponent(u_unit[n]) - 100);
         e = min(max(e, 2), 252);
         next[n] = __uint_as_float(static_cast<uint32_t>(e) << 23);
         const float up = __uint_as_float(static_cast<uint32_t>(254 - e) << 23);
-        keep[n] = left * up;
+        keep[n] = __builtin_ldexpf(decay, unit - e);
         bound[n] = bound[n] * keep[n] + 64.f * (most * up);
-        const float unit = u_unit[n] * up;
-        split(end[0] * unit, end[1] * unit, u_hi[n], u_lo[n]);
+        const float to = u_unit[n] * up;
+        split(end[0] * to, end[1] * to, u_hi[n], u_lo[n]);
         if (OUT) {
           const Scale sc = scale_of(max_of_rows(all) * u_unit[n]);
           w_unit[n] = sc.down;

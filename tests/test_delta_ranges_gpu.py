@@ -113,3 +113,20 @@ def test_large_values_before_a_reset(dtype, size):
     d["g"][20] = -np.inf
     _run(d, [420], bar_tokens=100)
     _run(d, [50, 370], bar_tokens=100)
+
+
+@pytest.mark.parametrize("total", [-0.01, -3.0, -20.0, -60.0, -80.0])
+def test_a_state_that_only_decays(total):
+    """hT = e^(sum of g) h0 with closed gates: one exponential (an instruction good to
+    2^-23 of a fraction rounded to 2^-25) and one product (2^-24; of numbers below
+    2^-126 a step of 2^-149)."""
+    g = torch.Generator().manual_seed(114)
+    d = delta_inputs(32, 1, 2, 64, 64, 115)
+    d["beta"][:] = 0.0
+    part = torch.rand((32, 2), generator=g)
+    d["g"] = (total * part / part.sum(0)).float().contiguous()
+    h0 = torch.randn((1, 2, 64, 64), generator=g)
+    c = on_gpu(d)
+    _, hT = P.delta(c["q"], c["k"], c["v"], c["g"], c["beta"], h0.to(DEV), starts=starts_of([32]).to(DEV), qk_norm=True)
+    ref = h0.double() * d["g"].double().sum(0).exp()[None, :, None, None]
+    assert bool(((hT.cpu().double() - ref).abs() <= 2.0 ** -21 * ref.abs() + 2.0 ** -149).all())
