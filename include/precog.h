@@ -582,11 +582,10 @@ size_t precog_delta_workspace_bytes(const precog_delta_desc *desc, int packed);
  *              (then q is not read and may be NULL).
  *   hT         state rows like h0, or NULL.  May equal h0 exactly without
  *              h0_idx (in place); must not overlap h0 otherwise.
- * Arithmetic: states, sums, decays and norms in fp32; the products of blocks
- * of 32 tokens run on the matrix cores with operands of 22 bits (o too, which is
- * rounded to its type at the end), counted from the largest of a column and block:
- * where beta |k|^2 > 2 lets the rule expand, a block's small results are good
- * to 2^-20 of its large ones.  With norms of 2^63 and more the sum of squares
+ * Arithmetic: states, sums, decays, norms and the products between the tokens of
+ * a block of 32 in fp32; the products with states run on the matrix cores with
+ * operands of 22 bits, counted from the largest element of the state's column (o
+ * too, which is rounded to its type at the end). With norms of 2^63 and more the sum of squares
  * leaves fp32.  A NaN or an infinity in a token reaches o of its head and
  * sequence from the beginning of the token's block of 32 on.
  *   workspace  precog_delta_workspace_bytes(desc, starts != NULL) bytes; NULL

@@ -34,15 +34,16 @@
 // or row 4 q + j - 4 of the second, and the other operand is laid out to match.
 //
 // Numbers.  The states, all sums, decays and norms are fp32 (b is summed in
-// fp64, where the differences of two positions are taken).  A product's
-// operands are fp16: keys and queries under the power of two that brings the
-// row's norm to [1, 2) (exact for bf16 down to 2^-16 of it, good to 2^-25; fp32
-// inputs as two halves of 11 bits; queries under 2^12 more, which leaves G . Q K^T
-// its 22 bits under decays down to e^-9), and S, X, U and T as two halves (22 bits)
-// under a power of two of their own, a column's (T: a block's): X, T and the U of
-// O have their largest at 2^14, S and its U are held below 2^16 and 2^8.  Products of two low halves are left out (2^-22).  A
-// bf16 o is computed as an fp32 one and rounded at the end: its two terms may
-// cancel, as they do where a value is replaced.  Errors against 64 bits over
+// fp64, where the differences of two positions are taken), and so are T, X, U and
+// G . Q K^T with their products: the tokens of a block differ by what decays, gates,
+// values and key lengths make of them, and a token's small numbers are not to
+// depend on its neighbours' large ones.  The products with S and K have operands of
+// fp16: keys and queries under the power of two that brings the row's norm to [1, 2)
+// (exact for bf16 down to 2^-16 of it, good to 2^-25; fp32 inputs as two halves of 11
+// bits), S and the U that goes into it as two halves (22 bits) under a power of two
+// of their column's, below 2^16 and 2^8.  Products of two low halves are left out
+// (2^-22).  A bf16 o is computed as an fp32 one and rounded at the end: its two terms
+// may cancel, as they do where a value is replaced.  Errors against 64 bits over
 // 40,001 tokens: states 2.2e-7, as a plain evaluation in 32 bits (two bf16
 // halves: 16 bits, some 3e-6 by that).
 //
@@ -67,10 +68,8 @@ namespace {
 
 constexpr int kBlockTokens = 32;
 constexpr int kChainMax = 4;     // chain waves of a workgroup
-constexpr float kQueryUp = 4096.f;  // power of two of queries above that of keys
 
 typedef _Float16 half8 __attribute__((ext_vector_type(8)));
-typedef _Float16 half4 __attribute__((ext_vector_type(4)));
 typedef _Float16 half2 __attribute__((ext_vector_type(2)));
 typedef float float2v __attribute__((ext_vector_type(2)));
 typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
@@ -86,19 +85,16 @@ struct Factors {
   float q[kBlockTokens];   // scale |q| e^b of Q S
   float o[kBlockTokens];   // scale |q| of Q K^T U
   float decay;             // e^{b_end}
-  float t;                 // power of two that T's operand lacks
-  float pad[2];
+  float pad[3];
 };
 
 // What a call computes beside the states.
 constexpr int kNoOutput = 0, kOut16 = 1, kOut32 = 2;
 
-// A lower triangle of 32 x 32 numbers as two halves of operands: the rows of the
-// first token tile, whose depths 4 q + j are its own tokens, and of the second.
-struct Lower {
-  half4 first[2][64];
-  half8 second[2][64];
-};
+// A lower triangle of 32 x 32 numbers as operands of v_mfma_f32_16x16x4_f32: the tiles
+// (0, 0), (1, 0) and (1, 1); lane l has the columns 4 (l / 16) .. + 3 of row l % 16.
+// Step r multiplies those of register r, as a result's register r holds its rows.
+using Lower = float4v[3][64];
 
 // A block's operands in LDS, in 1 KB fragments of one matrix instruction.
 template <int KP, bool IN32, int OUT>
@@ -122,8 +118,8 @@ struct Scratch {
   float beta[kBlockTokens];   // beta |k|^2
 };
 
-// A and its inverse take the place of T's operands until these are made: three
-// tiles of 16 x 16 floats, (0, 0), (1, 0) and (1, 1).  Groups of four columns are
+// A and its inverse take the place of T's operands until these are made, tile by
+// tile.  Groups of four columns are
 // permuted within a row, so that 16 lanes that read a column of groups meet
 // different banks, and neighbouring rows of the last tile change places, so that
 // a row of it and the same one of the first do.
@@ -131,7 +127,6 @@ __device__ __forceinline__ int a_at(int row, int col) {
   const int tile = row / 16 + col / 16, r = row % 16, c = col % 16;
   return 256 * tile + 16 * (r ^ (tile == 2)) + 4 * (c / 4 ^ r / 4) + c % 4;
 }
-static_assert(sizeof(Lower) == 3 * 256 * sizeof(float), "A's tiles");
 
 template <int KP, bool IN32, int OUT>
 struct Shared {
@@ -146,9 +141,6 @@ struct Shared {
 
 __device__ __forceinline__ float4v mfma(half8 a, half8 b, float4v c) {
   return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0);
-}
-__device__ __forceinline__ float4v mfma(half4 a, half4 b, float4v c) {
-  return __builtin_amdgcn_mfma_f32_16x16x16f16(a, b, c, 0, 0, 0);
 }
 __device__ __forceinline__ float4v mfma(float a, float b, float4v c) {
   return __builtin_amdgcn_mfma_f32_16x16x4f32(a, b, c, 0, 0, 0);
@@ -201,7 +193,7 @@ __device__ __forceinline__ float less_half(float x, half2 h) {
   return d;
 }
 
-// Eight fp32 values as halves of 11 bits each, or four.
+// Eight fp32 values as halves of 11 bits each.
 __device__ __forceinline__ void split(const float4v& a, const float4v& b, half8& hi, half8& lo) {
   half2 h[4], l[4];
 #pragma unroll
@@ -213,16 +205,6 @@ __device__ __forceinline__ void split(const float4v& a, const float4v& b, half8&
   hi = half8{h[0][0], h[0][1], h[1][0], h[1][1], h[2][0], h[2][1], h[3][0], h[3][1]};
   lo = half8{l[0][0], l[0][1], l[1][0], l[1][1], l[2][0], l[2][1], l[3][0], l[3][1]};
 }
-__device__ __forceinline__ void split(const float4v& a, half4& hi, half4& lo) {
-  const half2 h0 = to_half2(a[0], a[1]), h1 = to_half2(a[2], a[3]);
-  const half2 l0 = to_half2(less_half<0>(a[0], h0), less_half<1>(a[1], h0));
-  const half2 l1 = to_half2(less_half<0>(a[2], h1), less_half<1>(a[3], h1));
-  hi = half4{h0[0], h0[1], h1[0], h1[1]};
-  lo = half4{l0[0], l0[1], l1[0], l1[1]};
-}
-// The depths of the first token tile.
-__device__ __forceinline__ half4 first_tile(const half8& v) { return __builtin_shufflevector(v, v, 0, 1, 2, 3); }
-
 // 2^x.  The integer part by itself: in fp32 2^-90 would be good to 2^-18.
 __device__ __forceinline__ float exp2_of(double x) {
   const double whole = rint(x);
@@ -342,11 +324,10 @@ __device__ __forceinline__ float row_factor(float sq, int norm, float eps) {
   return norm ? down * __builtin_amdgcn_rsqf(sq + eps) : down;
 }
 
-// Rows times `more` as operands in LDS (and, for keys, transposed ones), and every
-// token's sum of squares.
+// Rows as operands in LDS (and, for keys, transposed ones), and every token's
+// sum of squares.
 template <int KP, bool IN32, bool TRANSPOSE, typename TIn, typename Frags, typename FragsT>
-__device__ __forceinline__ void make_operand(const Rows<KP, TIn>& rows, Frags& frags, FragsT& turned, float* squares,
-                                             float more) {
+__device__ __forceinline__ void make_operand(const Rows<KP, TIn>& rows, Frags& frags, FragsT& turned, float* squares) {
   using R = Rows<KP, TIn>;
   const int lane = fresh_lane(), c = lane % R::kLanes, row = lane / 16;
 #pragma unroll
@@ -355,7 +336,7 @@ __device__ __forceinline__ void make_operand(const Rows<KP, TIn>& rows, Frags& f
     float v[8];
     rows.values(i, v);
     const float sq = row_sum<KP>(rows.squares(i, v));
-    const float up = row_scale(sq).up * more;
+    const float up = row_scale(sq).up;
     if (c == 0) squares[4 * lp + row] = sq;
     uint32_t word[2][4];
 #pragma unroll
@@ -436,15 +417,15 @@ __device__ __forceinline__ void prepare_block(const DeltaParams& p, Inputs<KP, O
     const double up = __shfl_up(b, d, kBlockTokens);
     if (lane % kBlockTokens >= d) b += up;
   }
-  make_operand<KP, IN32, true, TIn>(in.k, buf.k, buf.kt, s.rk, 1.f);
-  if constexpr (outputs) make_operand<KP, IN32, false, TIn>(in.q, buf.q, buf.kt, s.rq, kQueryUp);
+  make_operand<KP, IN32, true, TIn>(in.k, buf.k, buf.kt, s.rk);
+  if constexpr (outputs) make_operand<KP, IN32, false, TIn>(in.q, buf.q, buf.kt, s.rq);
   wave_fence();
   // lane l has token l % 32 (a token behind the last one has no key and no query;
   // a key of zeros has no length either, so its value does not reach X)
   const bool live = lane % kBlockTokens < in.rows;
   const float sq = s.rk[lane % kBlockTokens];
   const float rk = live && sq != 0.f ? row_factor(sq, p.norm, p.eps) : 0.f;
-  const float rq = live && outputs ? row_factor(s.rq[lane % kBlockTokens], p.norm, p.eps) / kQueryUp : 0.f;
+  const float rq = live && outputs ? row_factor(s.rq[lane % kBlockTokens], p.norm, p.eps) : 0.f;
   const double b2 = b * 1.4426950408889634;
   const float gate = in.beta * rk;
   if (lane < kBlockTokens) {
@@ -512,8 +493,8 @@ __device__ __forceinline__ void prepare_block(const DeltaParams& p, Inputs<KP, O
     *reinterpret_cast<float4v*>(&A[a_at(row, cols)]) = a;
   }
   if constexpr (outputs) {
-    split(pm[0], buf.p[0].first[0][lane], buf.p[0].first[1][lane]);
-    split(pm[1], pm[2], buf.p[0].second[0][lane], buf.p[0].second[1][lane]);
+#pragma unroll
+    for (int i = 0; i < 3; ++i) buf.p[0][i][lane] = pm[i];
   }
   wave_fence();
 
@@ -563,14 +544,10 @@ __device__ __forceinline__ void prepare_block(const DeltaParams& p, Inputs<KP, O
   {
     const float4v t11 = *reinterpret_cast<const float4v*>(&A[a_at(m, 4 * q)]);
     const float4v t21 = *reinterpret_cast<const float4v*>(&A[a_at(16 + m, 4 * q)]);
-    float most = 0.f;
-#pragma unroll
-    for (int r = 0; r < 4; ++r) most = max_abs(max_abs(max_abs(most, t11[r]), t21[r]), t22[r]);
-    const float t_most = wave_max(most);
-    const Scale sc = scale_of(t_most);
     wave_fence();  // A has been read
-    split(t11 * sc.up, buf.t.first[0][lane], buf.t.first[1][lane]);
-    split(t21 * sc.up, t22 * sc.up, buf.t.second[0][lane], buf.t.second[1][lane]);
+    buf.t[0][lane] = t11;
+    buf.t[1][lane] = t21;
+    buf.t[2][lane] = t22;
     const float fo = p.scale * rq;
     const float eb = exp2_of(b2);
     const float fu = exp2_of(readlane_d(b2, kBlockTokens - 1) - b2);
@@ -581,9 +558,6 @@ __device__ __forceinline__ void prepare_block(const DeltaParams& p, Inputs<KP, O
       buf.f.q[lane] = fo * eb;
       buf.f.o[lane] = fo;
       if (lane == kBlockTokens - 1) buf.f.decay = eb;
-      if (lane == 0) {
-        buf.f.t = sc.down;
-      }
     }
   }
   wave_fence();
@@ -627,17 +601,21 @@ __device__ __forceinline__ void store_cols(__amdgpu_buffer_rsrc_t r, uint32_t of
   }
 }
 
-// A lower triangle times 32 tokens of 16 columns, which are two halves.
-__device__ __forceinline__ void by_lower(const Lower& a, int lane, const half8& hi, const half8& lo, float4v& top,
-                                         float4v& bottom) {
-  const half4 a_hi = a.first[0][lane], a_lo = a.first[1][lane];
-  const half8 b_hi = a.second[0][lane], b_lo = a.second[1][lane];
-  top = mfma(a_hi, first_tile(hi), top);
-  bottom = mfma(b_hi, hi, bottom);
-  top = mfma(a_hi, first_tile(lo), top);
-  bottom = mfma(b_hi, lo, bottom);
-  top = mfma(a_lo, first_tile(hi), top);
-  bottom = mfma(b_lo, hi, bottom);
+// A lower triangle times 32 tokens of 16 NV columns.
+template <int NV>
+__device__ __forceinline__ void by_lower(const Lower& a, int lane, const float4v (&x)[2][NV], float4v (&out)[2][NV]) {
+  const float4v t00 = a[0][lane], t10 = a[1][lane], t11 = a[2][lane];
+#pragma unroll
+  for (int r = 0; r < 4; ++r)
+#pragma unroll
+    for (int n = 0; n < NV; ++n) {
+      out[0][n] = mfma(t00[r], x[0][n][r], out[0][n]);
+      out[1][n] = mfma(t10[r], x[0][n][r], out[1][n]);
+    }
+#pragma unroll
+  for (int r = 0; r < 4; ++r)
+#pragma unroll
+    for (int n = 0; n < NV; ++n) out[1][n] = mfma(t11[r], x[1][n][r], out[1][n]);
 }
 
 // The states of a wave's columns: row r of tile t is the state row 32 (t / 2) +
@@ -885,9 +863,8 @@ __global__ void __launch_bounds__(64 * (kChainMax + Shared<KP, IN32, OUT>::kPrep
         }
       }
     }
-    // X, then U = T X without the powers of two of their operands
+    // X, then U = T X
     float4v u[2][NV] = {};
-    float u_unit[NV];
     {
       float4v x[2][NV];
 #pragma unroll
@@ -900,26 +877,11 @@ __global__ void __launch_bounds__(64 * (kChainMax + Shared<KP, IN32, OUT>::kPrep
           for (int r = 0; r < 4; ++r) x[t][n][r] = fv[r] * col_value<TIn>(raw[t][r], n) - fx[r] * sigma[n] * ks[t][n][r];
       }
       if (c + 1 < blocks) fetch(c + 1);
-      half8 x_hi[NV], x_lo[NV];
-#pragma unroll
-      for (int n = 0; n < NV; ++n) {
-        float most = 0.f;
-#pragma unroll
-        for (int t = 0; t < 2; ++t)
-#pragma unroll
-          for (int r = 0; r < 4; ++r) most = max_abs(most, x[t][n][r]);
-        most = max_of_rows(most);
-        const Scale sc = scale_of(most);
-        u_unit[n] = sc.down * buf.f.t;
-        split(x[0][n] * sc.up, x[1][n] * sc.up, x_hi[n], x_lo[n]);
-      }
-#pragma unroll
-      for (int n = 0; n < NV; ++n) by_lower(buf.t, lane, x_hi[n], x_lo[n], u[0][n], u[1][n]);
+      by_lower<NV>(buf.t, lane, x, u);
     }
-    // U / sigma' under its decays for K^T, and U under a power of two of its own
-    // for Q K^T
-    half8 u_hi[NV], u_lo[NV], w_hi[NV], w_lo[NV];
-    float next[NV], keep[NV], w_unit[NV];  // sigma', the factor of S~, what U for Q K^T lacks
+    // U / sigma' under its decays, for K^T
+    half8 u_hi[NV], u_lo[NV];
+    float next[NV], keep[NV];  // sigma', and the factor of S~
     {
       float4v fu[2];
 #pragma unroll
@@ -928,35 +890,23 @@ __global__ void __launch_bounds__(64 * (kChainMax + Shared<KP, IN32, OUT>::kPrep
 #pragma unroll
       for (int n = 0; n < NV; ++n) {
         const float4v end[2] = {u[0][n] * fu[0], u[1][n] * fu[1]};
-        float most = 0.f, all = 0.f;
+        float most = 0.f;
 #pragma unroll
         for (int t = 0; t < 2; ++t)
 #pragma unroll
-          for (int r = 0; r < 4; ++r) {
-            most = max_abs(most, end[t][r]);
-            all = max_abs(all, u[t][n][r]);
-          }
-        most = max_of_rows(most) * u_unit[n];
-        // exponents of sigma' for U, for S~, and the least, where both vanish (the
-        // last one of all keeps U's factor in fp32)
+          for (int r = 0; r < 4; ++r) most = max_abs(most, end[t][r]);
+        most = max_of_rows(most);
+        // exponents of sigma' for U, for S~, and the least, where both vanish
         const int unit = exponent(sigma[n]);
         int e = exponent(most) - 7;
         e = max(e, exponent(bound[n] * decay) + unit - 127 - 13);
         e = max(e, exponent(decay) + unit - 127 - 64);
-        e = max(e, exponent(u_unit[n]) - 100);
         e = min(max(e, 2), 252);
         next[n] = __uint_as_float(static_cast<uint32_t>(e) << 23);
         const float up = __uint_as_float(static_cast<uint32_t>(254 - e) << 23);
         keep[n] = __builtin_ldexpf(decay, unit - e);
         bound[n] = bound[n] * keep[n] + 64.f * (most * up);
-        const float to = u_unit[n] * up;
-        split(end[0] * to, end[1] * to, u_hi[n], u_lo[n]);
-        if (OUT) {
-          const Scale sc = scale_of(max_of_rows(all) * u_unit[n]);
-          w_unit[n] = sc.down;
-          const float own = u_unit[n] * sc.up;
-          split(u[0][n] * own, u[1][n] * own, w_hi[n], w_lo[n]);
-        }
+        split(end[0] * up, end[1] * up, u_hi[n], u_lo[n]);
       }
     }
 #pragma unroll
@@ -975,8 +925,10 @@ __global__ void __launch_bounds__(64 * (kChainMax + Shared<KP, IN32, OUT>::kPrep
           make_rsrc(o_at, (rows_of(c) - 1) * o_step + p.V * static_cast<uint32_t>(sizeof(TOut)));
       o_at += static_cast<int64_t>(kBlockTokens) * p.Hv * p.V;
       float4v pu[2][NV] = {};
-#pragma unroll
-      for (int n = 0; n < NV; ++n) by_lower(buf.p[0], lane, w_hi[n], w_lo[n], pu[0][n], pu[1][n]);
+      // not among the products that the next block waits for
+      __builtin_amdgcn_sched_barrier(0);
+      by_lower<NV>(buf.p[0], lane, u, pu);
+      __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
       for (int t = 0; t < 2; ++t) {
         const float4v fq = *reinterpret_cast<const float4v*>(&buf.f.q[16 * t + 4 * q]);
@@ -986,7 +938,7 @@ __global__ void __launch_bounds__(64 * (kChainMax + Shared<KP, IN32, OUT>::kPrep
           float v[NV];
 #pragma unroll
           for (int n = 0; n < NV; ++n)
-            v[n] = fq[r] * (sigma[n] * qs[t][n][r]) + fo[r] * (w_unit[n] * pu[t][n][r]);
+            v[n] = fq[r] * (sigma[n] * qs[t][n][r]) + fo[r] * pu[t][n][r];
           store_cols<TOut, NV>(ro, o_off + (16 * t + r) * o_step, v);
         }
       }

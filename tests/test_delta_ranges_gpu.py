@@ -130,3 +130,63 @@ def test_a_state_that_only_decays(total):
     _, hT = P.delta(c["q"], c["k"], c["v"], c["g"], c["beta"], h0.to(DEV), starts=starts_of([32]).to(DEV), qk_norm=True)
     ref = h0.double() * d["g"].double().sum(0).exp()[None, :, None, None]
     assert bool(((hT.cpu().double() - ref).abs() <= 2.0 ** -21 * ref.abs() + 2.0 ** -149).all())
+
+
+@pytest.mark.parametrize("dtype", IO)
+@pytest.mark.parametrize("size", [1e6, 1e8, 1e12])
+@pytest.mark.parametrize("g", [-np.inf, -40.0])
+def test_very_large_values_before_a_reset(dtype, size, g):
+    d = delta_inputs(420, 1, 2, 64, 64, 131, dtype, sliced=False)
+    d["v"][5] = (d["v"][5].float() * size).to(dtype)
+    d["g"][20] = g
+    _run(d, [420], bar_tokens=100)
+
+
+@pytest.mark.parametrize("dtype", IO)
+@pytest.mark.parametrize("out", IO)
+@pytest.mark.parametrize("g", [-16.0, -20.0, -30.0])
+@pytest.mark.parametrize("K,V", [(64, 64), (128, 40)])
+def test_outputs_behind_strong_decays(dtype, out, g, K, V):
+    """Tokens that forget in the middle of a block and at its end: o of the
+    tokens behind them in the same block, of the next block, and the states."""
+    d = delta_inputs(80, 1, 2, K, V, 132, dtype)
+    d["g"][12] = d["g"][31] = g
+    d["beta"][12:32] = 0.0
+    d["beta"][32:60] = 0.0
+    d["g"][32:] *= 0.1
+    _run(d, [80], out=out)
+    _run({x: t[:32] for x, t in d.items()}, [32], out=out)
+
+
+@pytest.mark.parametrize("dtype", IO)
+def test_heads_that_forget_fast(dtype):
+    """Ordinary values under log decays of -0.1 to -3 a token."""
+    d = delta_inputs(300, 2, 8, 64, 64, 133, dtype, rate=(0.1, 3.0))
+    _run(d, [300])
+    _run(d, [300], out=torch.bfloat16)
+
+
+@pytest.mark.parametrize("dtype", IO)
+@pytest.mark.parametrize("size", [1.0, 1e8])
+def test_resets_in_segments(dtype, size):
+    """The same in a call that is cut in time."""
+    d = delta_inputs(2400, 1, 1, 64, 64, 134, dtype, sliced=False)
+    at = torch.arange(5, 2400, 150)
+    d["v"][at] = (d["v"][at].float() * size).to(dtype)
+    d["g"][at + 9] = -40.0
+    d["beta"][at + 9] = 0.0
+    assert P.delta_workspace_bytes(P.delta_desc(1, 2400, 1, 1, 64, 64), True) > 0
+    _run(d, [2400], bar_tokens=200)
+
+
+@pytest.mark.parametrize("dtype", IO)
+@pytest.mark.parametrize("g", [-10.0, -11.0, -12.0, -14.0, -20.0, -30.0])
+def test_blocks_that_end_in_strong_decay(dtype, g):
+    """As test_blocks_that_end_in_decay; the span between the block's decays on
+    both sides of what two halves take."""
+    d = delta_inputs(72, 1, 2, 64, 64, 135, dtype)
+    d["g"][31] = g
+    d["beta"][31:] = 0.0
+    d["g"][32:] = 0.0
+    _run(d, [72])
+    _run({x: t[:32] for x, t in d.items()}, [32])
