@@ -566,6 +566,9 @@ size_t precog_delta_workspace_bytes(const precog_delta_desc *desc, int packed);
  *   q, k       [B, L, k_heads, K], v [B, L, v_heads, V] in desc->in_dtype.
  *   g, beta    [B, L, v_heads] fp32, or NULL for g = 0 / beta = 1.  g is the
  *              log decay; g below -256 (-infinity too) erases the state.
+ *              g > 0 lets the state grow; where the sum of g over consecutive
+ *              tokens passes 88, e to it leaves fp32, and o and the state of
+ *              the head may be infinite or NaN.
  *   starts     NULL, or [B + 1] int32 on the device: the sequences then lie
  *              one behind the other in q, k, v, g, beta and o of T tokens,
  *              sequence b in [starts[b], starts[b+1]), of any length (0 too).
@@ -585,9 +588,9 @@ size_t precog_delta_workspace_bytes(const precog_delta_desc *desc, int packed);
  * Arithmetic: states, sums, decays, norms and the products between the tokens of
  * a block of 32 in fp32; the products with states run on the matrix cores with
  * operands of 22 bits, counted from the largest element of the state's column (o
- * too, which is rounded to its type at the end). With norms of 2^63 and more the sum of squares
- * leaves fp32.  A NaN or an infinity in a token reaches o of its head and
- * sequence from the beginning of the token's block of 32 on.
+ * too, which is rounded to its type at the end).  With norms of 2^63 and more the
+ * sum of squares leaves fp32.  A NaN or an infinity in a token reaches o of its
+ * head and sequence from the beginning of the token's block of 32 on.
  *   workspace  precog_delta_workspace_bytes(desc, starts != NULL) bytes; NULL
  *              where that is 0.  Calls that may overlap need one each.
  * Alignment: pointers 16 bytes (g, beta, starts, h0_idx: 4), strides as above.

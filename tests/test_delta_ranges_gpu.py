@@ -190,3 +190,26 @@ def test_blocks_that_end_in_strong_decay(dtype, g):
     d["g"][32:] = 0.0
     _run(d, [72])
     _run({x: t[:32] for x, t in d.items()}, [32])
+
+
+@pytest.mark.parametrize("dtype", IO)
+@pytest.mark.parametrize("out", IO)
+@pytest.mark.parametrize("g", [0.35, 2.0, 12.0, 40.0])
+def test_growing_states(dtype, out, g):
+    """Log decays above zero, in every token or in single ones: o and the states
+    against the oracle, and o of single steps."""
+    d = delta_inputs(70, 1, 2, 64, 64, 141, dtype)
+    d["g"][:] = 0.0
+    if g < 5:
+        d["g"][8:40] = g
+    else:
+        d["g"][8] = d["g"][40] = g
+    _run(d, [70], out=out)
+    c = on_gpu(d)
+    o, hT = P.delta(c["q"], c["k"], c["v"], c["g"], c["beta"], starts=starts_of([70]).to(DEV), qk_norm=True)
+    states, slot = torch.zeros((1, 2, 64, 64), device=DEV), torch.zeros(1, dtype=torch.int32, device=DEV)
+    rows = [P.delta_step(*(c[n][t:t + 1] for n in ("q", "k", "v", "g", "beta")), states, slot, qk_norm=True)
+            for t in range(70)]
+    size, last = sizes(d, [70], norm=True)
+    near(torch.cat(rows), o.cpu().double().numpy(), size, 2 * delta_bar(70))
+    near(states, hT.cpu().double().numpy(), np.broadcast_to(last[:, :, None] / 8, hT.shape), 2 * delta_bar(70))
