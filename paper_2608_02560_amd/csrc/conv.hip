@@ -19,6 +19,8 @@ constexpr int kAhead = 4;                 // tokens loaded at a time
 constexpr int kRunMost = 32, kRunLeast = 8;  // tokens of a run
 constexpr int64_t kL2Bytes = 32LL << 20;  // of the 8 XCDs
 
+__device__ __forceinline__ int uniform(int v) { return __builtin_amdgcn_readfirstlane(v); }
+
 // Input j (0 = oldest) of the W - 1 before the first token of sequence b.
 template <typename TIn>
 __device__ __forceinline__ void tail_input(const ConvParams& p, int64_t b, int j, int64_t d,
@@ -130,7 +132,8 @@ __global__ void __launch_bounds__(64 * kConvWaves) __attribute__((amdgpu_waves_p
   const int64_t first = static_cast<int64_t>(blockIdx.x) * run;
   const int64_t last = first + run < p.T ? first + run : p.T;
 
-  // the last sequence that begins at or before the run's first token
+  // the last sequence that begins at or before the run's first token (if starts
+  // ascend: any one if not)
   int64_t b = 0;
   if (p.starts == nullptr) {
     b = first / p.L;
@@ -147,18 +150,48 @@ __global__ void __launch_bounds__(64 * kConvWaves) __attribute__((amdgpu_waves_p
   const TIn* x = static_cast<const TIn*>(p.x) + d;
   TOut* y = static_cast<TOut*>(p.y) + d;
 
-  for (int64_t t = first; b < p.B; ++b) {
-    const Span span = sequence(p.starts, b, p.L, p.T);
-    if (span.begin >= last) break;
-    if (t < span.begin) t = span.begin;
+  // The sequences in their order, while each begins where the one before has ended.
+  // What is left of the run then, tokens of no sequence or of one that descending
+  // starts have put elsewhere, is sought in all of them, one a lane.
+  const int lane = threadIdx.x % 64;
+  const int64_t rest = (p.D - d) / kLaneCh + lane;  // lanes of the wave that are on: those below it
+  const int lanes = uniform(rest < 64 ? static_cast<int>(rest) : 64);
+  bool in_order = true;
+  int64_t reached = first;
+  int sought = 0, base = 0;
+  uint64_t found = 0;
+  for (;;) {
+    Span span = {0, 0};
+    int64_t seq = b;
+    if (in_order) {
+      if (reached >= last) break;
+      if (b < p.B) span = sequence(p.starts, b, p.L, p.T);
+      const bool holds = span.begin <= reached && reached < span.end;
+      in_order = holds || (b < p.B && span.begin == reached);  // (an empty one)
+      ++b;
+      if (!holds) continue;
+    } else {
+      while (found == 0 && sought < p.B) {
+        Span any = {0, 0};
+        if (sought + lane < p.B) any = sequence(p.starts, sought + lane, p.L, p.T);
+        found = __ballot(any.begin < any.end && any.begin < last && any.end > reached);
+        base = sought;
+        sought += lanes;
+      }
+      if (found == 0) break;
+      seq = base + __builtin_ctzll(found);
+      found &= found - 1;
+      span = sequence(p.starts, seq, p.L, p.T);
+    }
+    int64_t t = span.begin > reached ? span.begin : reached;
     const int64_t stop = span.end < last ? span.end : last;
-    if (t >= stop) continue;
+    if (in_order) reached = stop;
     float win[W - 1][kLaneCh];
 #pragma unroll
     for (int j = 0; j < W - 1; ++j) {
       const int64_t back = t - (W - 1) + j;
       if (back < span.begin) {
-        tail_input<TIn>(p, b, static_cast<int>(back - span.begin + W - 1), d, win[j]);
+        tail_input<TIn>(p, seq, static_cast<int>(back - span.begin + W - 1), d, win[j]);
       } else {
         const Pack<TIn, kLaneCh> v = load_pack<kLaneCh>(x + back * p.x_stride);
 #pragma unroll
@@ -180,7 +213,6 @@ __global__ void __launch_bounds__(64 * kConvWaves) __attribute__((amdgpu_waves_p
         }
       }
     }
-    t = stop;
   }
 }
 
