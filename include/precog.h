@@ -594,6 +594,8 @@ size_t precog_delta_workspace_bytes(const precog_delta_desc *desc, int packed);
  *   workspace  precog_delta_workspace_bytes(desc, starts != NULL) bytes; NULL
  *              where that is 0.  Calls that may overlap need one each.
  * Alignment: pointers 16 bytes (g, beta, starts, h0_idx: 4), strides as above.
+ * Sizes: as one launch's threads are counted in 32 bits, batch * v_heads *
+ * ceil(v_dim / 128) of 2^23 and more may be refused (PRECOG_ERR_SHAPE).
  * Deterministic; nothing but o, hT and the workspace is written. */
 precog_status precog_delta_encode(const precog_delta_desc *desc, const void *q,
                                   const void *k, const void *v, const float *g,
@@ -614,7 +616,8 @@ precog_status precog_delta_encode(const precog_delta_desc *desc, const void *q,
  *              is (rows of a padded batch).  Rows with the same slot are
  *              applied in the order of the rows (F16 states rounded after
  *              each), as separate calls would.
- * All in fp32 except the storage types.  Deterministic. */
+ * B * v_heads * ceil(v_dim / 128) < 2^24.  All in fp32 except the storage types.
+ * Deterministic. */
 precog_status precog_delta_step(const precog_delta_desc *desc, const void *q,
                                 const void *k, const void *v, const float *g,
                                 const float *beta, void *states,
@@ -653,7 +656,8 @@ typedef struct {
  *              inputs; NULL = not captured.  May equal tail0 exactly without
  *              tail_idx; must not overlap it otherwise.
  * fp32 sums in the order of the taps.  y must not overlap x.  Pointers 16-byte
- * aligned (starts and tail_idx: 4). */
+ * aligned (starts and tail_idx: 4).  Tokens / 32 + batch of 2^24 and more may be
+ * refused (PRECOG_ERR_SHAPE). */
 precog_status precog_conv_encode(const precog_conv_desc *desc, const void *x,
                                  const float *w, const float *bias,
                                  const int32_t *starts, const void *tail0,
@@ -693,7 +697,7 @@ size_t precog_score_workspace_bytes(int64_t T, int64_t V, int64_t top);
  * +infinity has NaN in all its numbers and ids of -1.  Sums in fp32.
  *   workspace  precog_score_workspace_bytes(T, V, top) bytes; calls that may
  *              overlap need one each
- * T < 2^31, V <= 2^28; logits aligned as their type, workspace 16 bytes, others 4. */
+ * T < 2^24, V <= 2^28; logits aligned as their type, workspace 16 bytes, others 4. */
 precog_status precog_score_tokens(const void *logits, precog_dtype logits_dtype,
                                   int64_t T, int64_t V, int64_t row_stride,
                                   const int32_t *token, int64_t top,

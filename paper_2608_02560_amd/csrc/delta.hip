@@ -67,7 +67,7 @@ namespace precog {
 namespace {
 
 constexpr int kBlockTokens = 32;
-constexpr int kChainMax = 4;     // chain waves of a workgroup
+constexpr int kChainMax = kDeltaChainMax;
 
 typedef _Float16 half8 __attribute__((ext_vector_type(8)));
 typedef _Float16 half2 __attribute__((ext_vector_type(2)));
@@ -130,9 +130,10 @@ __device__ __forceinline__ int a_at(int row, int col) {
 
 template <int KP, bool IN32, int OUT>
 struct Shared {
-  // as many as fit into the 160 KB of a CU, up to five
-  static constexpr int kBuffers = IN32 ? (KP == 128 ? 2 : 4) : 5;
-  static constexpr int kPrepare = kBuffers - 1;   // prepare waves: each works on a buffer of its own
+  // as many as fit into the 160 KB of a CU, up to five; each prepare wave works on a
+  // buffer of its own
+  static constexpr int kPrepare = delta_prepare_waves(IN32, KP == 128);
+  static constexpr int kBuffers = kPrepare + 1;
   Buffer<KP, IN32, OUT> buf[kBuffers];
   Scratch scratch[kPrepare];
   int ready[kBuffers];       // block held by the buffer, counted from 1

@@ -26,6 +26,9 @@ bool overlap(const void* a, size_t an, const void* b, size_t bn) {
   return an && bn && x < y + bn && y < x + an;
 }
 
+// A launch holds fewer than 2^32 threads.
+bool launchable(int64_t workgroups, int64_t threads) { return workgroups <= 0xffffffffLL / threads; }
+
 // Status of a finished launch.
 precog_status launched(hipError_t e) { return e == hipSuccess ? PRECOG_OK : PRECOG_ERR_HIP; }
 
@@ -98,6 +101,14 @@ int64_t delta_segments(const precog_delta_desc* d, int64_t tokens) {
   if (n > 32) n = 32;
   if (n > blocks / 16) n = blocks / 16;
   return n < 4 ? 1 : n;
+}
+
+// Whether a call's heads fit one launch: workgroups of up to 128 columns.
+bool delta_launchable(const precog_delta_desc* d) {
+  const int64_t columns = (d->v_dim + 31) / 32;
+  const int64_t waves = columns < precog::kDeltaChainMax ? columns : precog::kDeltaChainMax;
+  const int64_t prepare = precog::delta_prepare_waves(d->in_dtype == PRECOG_F32, d->k_dim > 64);
+  return launchable(d->batch * d->v_heads * ((columns + waves - 1) / waves), 64 * (waves + prepare));
 }
 
 struct DeltaWs {
@@ -238,6 +249,7 @@ precog_status precog_delta_encode(const precog_delta_desc* desc, const void* q, 
     p.between = static_cast<float*>(workspace);
     p.phi = reinterpret_cast<float*>(static_cast<char*>(workspace) + ws.between);
   }
+  if (!delta_launchable(desc)) return PRECOG_ERR_SHAPE;
   int cus = 1;
   st = precog::check_device(&cus);
   if (st != PRECOG_OK) return st;
@@ -259,6 +271,7 @@ precog_status precog_delta_step(const precog_delta_desc* desc, const void* q, co
     if (!aligned(p, 16)) return PRECOG_ERR_ALIGN;
   if (!aligned(g, 4) || !aligned(beta, 4) || !aligned(slots, 4)) return PRECOG_ERR_ALIGN;
   if (state_rows == 0) return PRECOG_OK;  // no slot can name a row
+  if (!launchable(desc->batch * desc->v_heads * ((desc->v_dim + 127) / 128), 256)) return PRECOG_ERR_SHAPE;
 
   precog::DeltaParams p = delta_params(desc, q, k, v, g, beta, o);
   p.idx = slots;
@@ -306,6 +319,11 @@ precog_status precog_conv_encode(const precog_conv_desc* desc, const void* x, co
   p.tailT = tailT;
   p.L = L;
   p.T = tokens;
+  // runs of 32 tokens and the tails, which go by themselves in place
+  const int64_t runs = p.y ? (tokens + 31) / 32 : 0, tails = tailT ? B : 0;
+  const bool apart = tail0 && tail0 == tailT && runs > 0;
+  if (!launchable(apart ? (runs > tails ? runs : tails) : runs + tails, D > 1536 ? 256 : (D + 511) / 512 * 64))
+    return PRECOG_ERR_SHAPE;
   int cus = 1;
   st = precog::check_device(&cus);
   if (st != PRECOG_OK) return st;
@@ -363,6 +381,7 @@ precog_status precog_score_tokens(const void* logits, precog_dtype logits_dtype,
                         static_cast<const void*>(top_logprob)})
     if (!aligned(p, 4)) return PRECOG_ERR_ALIGN;
   const int64_t splits = score_splits(T, V);
+  if (!launchable(T * splits, 256)) return PRECOG_ERR_SHAPE;
   const ScoreWs ws = score_ws(T, splits, top);
   if (ws.total > 0 && (!workspace || workspace_bytes < ws.total)) return PRECOG_ERR_WORKSPACE;
 

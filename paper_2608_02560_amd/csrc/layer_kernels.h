@@ -9,6 +9,9 @@ namespace precog {
 
 constexpr int kDeltaMaxK = 128;
 constexpr int kDeltaMaxV = 256;
+constexpr int kDeltaChainMax = 4;  // chain waves of a workgroup of the delta rule, 32 columns each
+// Its prepare waves, one less than LDS has buffers: keys of up to 128 elements, or 64.
+constexpr int delta_prepare_waves(bool in32, bool k128) { return in32 ? (k128 ? 1 : 3) : 4; }
 constexpr float kDeltaErase = -256.f;  // log decays below it act as it: exp is 0 in fp32
 
 // One gated-delta call.  Strides in elements; tokens of sequence b are
