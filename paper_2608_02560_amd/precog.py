@@ -614,7 +614,16 @@ def gather(store, idx, out_dtype=None, stream=None):
 
 
 # The gated-delta layer and token scoring.  These wrappers check what the
-# library cannot see (types, shapes, strides and devices of the tensors).
+# library cannot see (types, shapes, strides and devices of the tensors).  They
+# have no backward pass, and refuse tensors whose gradient they would lose.
+def _forward_only(*tensors):
+    if torch.is_grad_enabled():
+        for t in tensors:
+            if t is not None and t.requires_grad:
+                raise ValueError("there is no backward pass: call under torch.no_grad(), or with "
+                                 "detached tensors")
+
+
 def _same(name, t, dtype, shape, device, contiguous=True):
     """t is a tensor of that type, shape and device (and contiguous), or a ValueError."""
     if t.dtype is dtype and t.shape == shape and t.get_device() == device and \
@@ -691,6 +700,7 @@ def _handle(stream, device):
 
 def _delta_args(q, k, v, g, beta, lead, out_dtype, state_dtype):
     dev = _device_of(k)
+    _forward_only(q, k, v, g, beta)
     if k.dim() != lead + 2 or v.dim() != lead + 2:
         raise ValueError("k and v must have %d axes" % (lead + 2))
     dtype = k.dtype
@@ -720,7 +730,8 @@ def delta(q, k, v, g=None, beta=None, h0=None, *, starts=None, h0_idx=None, qk_n
     packed [T, Hk, K] and [T, Hv, V]; g (log decay) and beta [..., Hv] fp32;
     h0 [B, Hv, K, V] or, with h0_idx [B] int32, a store [rows, Hv, K, V] whose
     rows h0_idx names the sequences start from.  q None with want_o False: the
-    states only.  hT: a tensor for the states (h0 itself: in place)."""
+    states only.  hT: a tensor for the states (h0 itself: in place).  Rows of o
+    whose token is in none of starts' sequences are not written."""
     lead = 2 if starts is None else 1
     if q is None and want_o:
         raise ValueError("o needs q")
@@ -739,6 +750,7 @@ def delta(q, k, v, g=None, beta=None, h0=None, *, starts=None, h0_idx=None, qk_n
         if h0 is None:
             raise ValueError("h0_idx needs a store h0")
     if h0 is not None:
+        _forward_only(h0)
         rows = h0.shape[0] if h0_idx is not None else B
         _same("h0", h0, state_dtype, (rows, Hv, K, V), dev)
     if hT is not None:
@@ -768,6 +780,7 @@ def delta_step(q, k, v, g, beta, states, slots, *, qk_norm=False, eps=1e-6, scal
     if q is None and want_o:
         raise ValueError("o needs q")
     n = k.shape[0]
+    _forward_only(states)
     _same("states", states, states.dtype, (states.shape[0], Hv, K, V), dev)
     _same("slots", slots, torch.int32, (n,), dev)
     desc = DeltaDesc(n, 1, Hk, Hv, K, V, *strides, 0, 0, *codes, 1 if qk_norm else 0, eps, scale)
@@ -781,6 +794,7 @@ def delta_step(q, k, v, g, beta, states, slots, *, qk_norm=False, eps=1e-6, scal
 
 def _conv_args(x, w, bias, lead, out_dtype):
     dev = _device_of(x)
+    _forward_only(x, w, bias)
     if x.dim() != lead + 1 or w.dim() != 2:
         raise ValueError("x must have %d axes and w two" % (lead + 1))
     D, W = x.shape[-1], w.shape[1]
@@ -796,7 +810,8 @@ def conv(x, w, bias=None, tail0=None, *, starts=None, tail_idx=None, silu=True, 
     """The short causal convolution; returns (y, tailT).  x [B, L, D], or with
     starts [B + 1] (int32) the packed [T, D]; w [D, W] and bias [D] fp32; tail0
     [B, W - 1, D], or with tail_idx [B] int32 a store of tails.  tailT: a tensor
-    for the tails (tail0 itself: in place)."""
+    for the tails (tail0 itself: in place).  Rows of y whose token is in none of
+    starts' sequences are not written."""
     lead = 2 if starts is None else 1
     out_dtype = out_dtype or x.dtype
     dev, D, W, codes, stride = _conv_args(x, w, bias, lead, out_dtype)
@@ -812,6 +827,7 @@ def conv(x, w, bias=None, tail0=None, *, starts=None, tail_idx=None, silu=True, 
         if tail0 is None:
             raise ValueError("tail_idx needs a store tail0")
     if tail0 is not None:
+        _forward_only(tail0)
         rows = tail0.shape[0] if tail_idx is not None else B
         _same("tail0", tail0, x.dtype, (rows, W - 1, D), dev)
     if tailT is not None:
@@ -835,6 +851,7 @@ def conv_step(x, w, bias, tails, slots, *, silu=True, out_dtype=None, stream=Non
     out_dtype = out_dtype or x.dtype
     dev, D, W, codes, stride = _conv_args(x, w, bias, 1, out_dtype)
     n = x.shape[0]
+    _forward_only(tails)
     _same("tails", tails, x.dtype, (tails.shape[0], W - 1, D), dev)
     _same("slots", slots, torch.int32, (n,), dev)
     desc = ConvDesc(n, 1, D, W, stride, *codes, 1 if silu else 0)
@@ -852,6 +869,7 @@ def score_tokens(logits, token=None, top=0, *, want_entropy=True, stream=None):
     (logprob [T], entropy [T], top_id [T, top], top_logprob [T, top]), None where
     not wanted."""
     dev = _device_of(logits)
+    _forward_only(logits)
     if logits.dim() != 2:
         raise ValueError("logits must be [T, V]")
     T, V = logits.shape
