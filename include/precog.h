@@ -549,7 +549,11 @@ typedef struct {
 
 /* Bytes of device workspace precog_delta_encode needs for this descriptor,
  * `packed` nonzero for a call with `starts`: 0 unless long sequences have few
- * heads, which are then computed in segments.  0 for a descriptor it refuses. */
+ * heads (at most 64 of batch * v_heads * ceil(v_dim / 128)), which are then
+ * computed in segments of 512 tokens and more.  That goes by the sequences' mean
+ * length: their lengths lie on the device, so one long sequence among many short
+ * ones, or among many heads, runs as a single chain of blocks (2.2 ms for 40,001
+ * tokens).  0 for a descriptor it refuses. */
 size_t precog_delta_workspace_bytes(const precog_delta_desc *desc, int packed);
 
 /* The gated delta rule: the second kind of layer whose state can be stored
