@@ -592,9 +592,10 @@ size_t precog_delta_workspace_bytes(const precog_delta_desc *desc, int packed);
  * Arithmetic: states, sums, decays, norms and the products between the tokens of
  * a block of 32 in fp32; the products with states run on the matrix cores with
  * operands of 22 bits, counted from the largest element of the state's column (o
- * too, which is rounded to its type at the end).  With norms of 2^63 and more the
- * sum of squares leaves fp32.  A NaN or an infinity in a token reaches o of its
- * head and sequence from the beginning of the token's block of 32 on.
+ * too, which is rounded to its type at the end).  Norms of keys and queries below
+ * 2^-62 or from 2^62 on leave fp32 when they are squared.  A NaN or an infinity in
+ * a token reaches o of its head and sequence from the beginning of the token's
+ * block of 32 on.
  *   workspace  precog_delta_workspace_bytes(desc, starts != NULL) bytes; NULL
  *              where that is 0.  Calls that may overlap need one each.
  * Alignment: pointers 16 bytes (g, beta, starts, h0_idx: 4), strides as above.

@@ -422,10 +422,12 @@ __device__ __forceinline__ void prepare_block(const DeltaParams& p, Inputs<KP, O
   if constexpr (outputs) make_operand<KP, IN32, false, TIn>(in.q, buf.q, buf.kt, s.rq);
   wave_fence();
   // lane l has token l % 32 (a token behind the last one has no key and no query;
-  // a key of zeros has no length either, so its value does not reach X)
+  // a key of zeros has no length either, so its value does not reach X, unless it is
+  // to be divided by a zero)
   const bool live = lane % kBlockTokens < in.rows;
   const float sq = s.rk[lane % kBlockTokens];
-  const float rk = live && sq != 0.f ? row_factor(sq, p.norm, p.eps) : 0.f;
+  const float length = row_factor(sq, p.norm, p.eps);
+  const float rk = live && (sq != 0.f || length == __builtin_inff()) ? length : 0.f;
   const float rq = live && outputs ? row_factor(s.rq[lane % kBlockTokens], p.norm, p.eps) : 0.f;
   const double b2 = b * 1.4426950408889634;
   const float gate = in.beta * rk;

@@ -213,3 +213,21 @@ def test_growing_states(dtype, out, g):
     size, last = sizes(d, [70], norm=True)
     near(torch.cat(rows), o.cpu().double().numpy(), size, 2 * delta_bar(70))
     near(states, hT.cpu().double().numpy(), np.broadcast_to(last[:, :, None] / 8, hT.shape), 2 * delta_bar(70))
+
+
+def test_a_zero_divided_by_a_zero_norm_is_nan():
+    """qk_norm with eps = 0 and a key or a query of zeros, in both entry points; with
+    an eps they are zeros."""
+    d = delta_inputs(3, 1, 1, 64, 64, 151, sliced=False)
+    for name in ("k", "q"):
+        for eps in (0.0, 1e-6):
+            c = {n: t.clone() for n, t in d.items()}
+            c[name][1] = 0
+            c = on_gpu(c)
+            state, slot = torch.zeros((1, 1, 64, 64), device=DEV), torch.zeros(1, dtype=torch.int32, device=DEV)
+            o, hT = P.delta(c["q"], c["k"], c["v"], c["g"], c["beta"], starts=starts_of([3]).to(DEV), qk_norm=True, eps=eps)
+            steps = [P.delta_step(*(c[n][t:t + 1] for n in ("q", "k", "v", "g", "beta")), state, slot, qk_norm=True,
+                                  eps=eps) for t in range(3)]
+            for got, one in ((o[1], steps[1][0]), (hT, state)):
+                assert torch.equal(torch.isnan(got), torch.isnan(one))
+            assert bool(torch.isnan(steps[1]).all()) == (eps == 0) and bool(torch.isnan(state).any()) == (name == "k" and eps == 0)
