@@ -134,7 +134,8 @@ __global__ void __launch_bounds__(kThreads) delta_step_kernel(DeltaParams p) {
     const int64_t th = t * p.Hv + h;
     float gt = p.g != nullptr ? p.g[th] : 0.f;
     gt = gt < kDeltaErase ? kDeltaErase : gt;
-    const float a = __expf(gt), beta = p.beta != nullptr ? p.beta[th] : 1.f;
+    // (expf, not 2^(g log2 e), whose rounded exponent is good to 2^-18 near -60)
+    const float a = expf(gt), beta = p.beta != nullptr ? p.beta[th] : 1.f;
     float u[4], o[4];
     if (on) {
       const Pack<TIn, 4> v =

@@ -231,3 +231,19 @@ def test_a_zero_divided_by_a_zero_norm_is_nan():
             for got, one in ((o[1], steps[1][0]), (hT, state)):
                 assert torch.equal(torch.isnan(got), torch.isnan(one))
             assert bool(torch.isnan(steps[1]).all()) == (eps == 0) and bool(torch.isnan(state).any()) == (name == "k" and eps == 0)
+
+
+@pytest.mark.parametrize("lo,hi", [(-0.1, 0.0), (-20.0, -10.0), (-80.0, -40.0), (10.0, 60.0)])
+def test_a_step_that_only_decays(lo, hi):
+    """States after one token with a closed gate: an exponential (2^-23) and a product
+    (2^-24; below 2^-126 a step of 2^-149)."""
+    n = 64
+    gen = torch.Generator().manual_seed(161)
+    d = delta_inputs(n, 1, 2, 64, 64, 162)
+    d["beta"][:] = 0.0
+    d["g"] = lo + (hi - lo) * torch.rand((n, 2), generator=gen)
+    states = torch.randn((n, 2, 64, 64), generator=gen)
+    c, s = on_gpu(d), states.to(DEV)
+    P.delta_step(c["q"], c["k"], c["v"], c["g"], c["beta"], s, torch.arange(n, dtype=torch.int32, device=DEV), qk_norm=True)
+    ref = states.double() * d["g"].double().exp()[:, :, None, None]
+    assert bool(((s.cpu().double() - ref).abs() <= 2.0 ** -21 * ref.abs() + 2.0 ** -149).all())
