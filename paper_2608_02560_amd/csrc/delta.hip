@@ -123,9 +123,8 @@ struct Scratch {
 // permuted within a row, so that 16 lanes that read a column of groups meet
 // different banks, and neighbouring rows of the last tile change places, so that
 // a row of it and the same one of the first do.
-__device__ __forceinline__ int a_at(int row, int col) {
-  const int tile = row / 16 + col / 16, r = row % 16, c = col % 16;
-  return 256 * tile + 16 * (r ^ (tile == 2)) + 4 * (c / 4 ^ r / 4) + c % 4;
+__device__ __forceinline__ uint32_t a_at(uint32_t tile, uint32_t r, uint32_t c) {
+  return 256 * tile + 16 * (r ^ tile / 2) + (4 * (c / 4 ^ r / 4) | c % 4);
 }
 
 template <int KP, bool IN32, int OUT>
@@ -493,7 +492,7 @@ __device__ __forceinline__ void prepare_block(const DeltaParams& p, Inputs<KP, O
       a[r] = ti > tj || row > cols + r ? v : 0.f;
       pm[i][r] = decay * qk[i][r];
     }
-    *reinterpret_cast<float4v*>(&A[a_at(row, cols)]) = a;
+    *reinterpret_cast<float4v*>(&A[a_at(i, m, 4 * q)]) = a;
   }
   if constexpr (outputs) {
 #pragma unroll
@@ -506,14 +505,14 @@ __device__ __forceinline__ void prepare_block(const DeltaParams& p, Inputs<KP, O
   q = lane / 16;
   // (I + A)^-1 of the two diagonal 16 x 16 blocks: lane l has column l % 16 of
   // block l / 16 (the upper lanes repeat the lower ones)
-  const int blk = q & 1;
+  const uint32_t diagonal = 2 * (q & 1);
   float col[16];
 #pragma unroll
   for (int i = 0; i < 16; ++i) {
     float sum = i == m ? 1.f : 0.f;
 #pragma unroll
     for (int j4 = 0; j4 < (i + 3) / 4; ++j4) {
-      const float4v a = *reinterpret_cast<const float4v*>(&A[a_at(16 * blk + i, 16 * blk + 4 * j4)]);
+      const float4v a = *reinterpret_cast<const float4v*>(&A[a_at(diagonal, i, 4 * j4)]);
 #pragma unroll
       for (int j = 0; j < 4; ++j)
         if (4 * j4 + j < i) sum -= a[j] * col[4 * j4 + j];
@@ -526,7 +525,7 @@ __device__ __forceinline__ void prepare_block(const DeltaParams& p, Inputs<KP, O
   wave_fence();
   if (lane < 32) {
 #pragma unroll
-    for (int i = 0; i < 16; ++i) A[a_at(16 * blk + i, 16 * blk + m)] = col[i];
+    for (int i = 0; i < 16; ++i) A[a_at(diagonal, i, m)] = col[i];
   }
   wave_fence();
   lane = fresh_lane();
@@ -536,17 +535,17 @@ __device__ __forceinline__ void prepare_block(const DeltaParams& p, Inputs<KP, O
   float4v y = {}, z = {};
 #pragma unroll
   for (int st = 0; st < 4; ++st)
-    y = mfma(A[a_at(16 + m, 4 * st + q)], A[a_at(4 * st + q, m)], y);
-  const float4v t22 = *reinterpret_cast<const float4v*>(&A[a_at(16 + m, 16 + 4 * q)]);
+    y = mfma(A[a_at(1, m, 4 * st + q)], A[a_at(0, 4 * st + q, m)], y);
+  const float4v t22 = *reinterpret_cast<const float4v*>(&A[a_at(2, m, 4 * q)]);
 #pragma unroll
   for (int st = 0; st < 4; ++st) z = mfma(t22[st], y[st], z);
   wave_fence();
 #pragma unroll
-  for (int r = 0; r < 4; ++r) A[a_at(16 + 4 * q + r, m)] = -z[r];
+  for (int r = 0; r < 4; ++r) A[a_at(1, 4 * q + r, m)] = -z[r];
   wave_fence();
   {
-    const float4v t11 = *reinterpret_cast<const float4v*>(&A[a_at(m, 4 * q)]);
-    const float4v t21 = *reinterpret_cast<const float4v*>(&A[a_at(16 + m, 4 * q)]);
+    const float4v t11 = *reinterpret_cast<const float4v*>(&A[a_at(0, m, 4 * q)]);
+    const float4v t21 = *reinterpret_cast<const float4v*>(&A[a_at(1, m, 4 * q)]);
     wave_fence();  // A has been read
     buf.t[0][lane] = t11;
     buf.t[1][lane] = t21;
