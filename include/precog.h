@@ -552,7 +552,7 @@ typedef struct {
  * heads (at most 64 of batch * v_heads * ceil(v_dim / 128)), which are then
  * computed in segments of 512 tokens and more.  That goes by the sequences' mean
  * length: their lengths lie on the device, so one long sequence among many short
- * ones, or among many heads, runs as a single chain of blocks (2.2 ms for 40,001
+ * ones, or among many heads, runs as a single chain of blocks (2.4 ms for 40,001
  * tokens).  0 for a descriptor it refuses. */
 size_t precog_delta_workspace_bytes(const precog_delta_desc *desc, int packed);
 

@@ -38,21 +38,22 @@
 // G . Q K^T with their products: the tokens of a block differ by what decays, gates,
 // values and key lengths make of them, and a token's small numbers are not to
 // depend on its neighbours' large ones.  The products with S and K have operands of
-// fp16: keys and queries under the power of two that brings the row's norm to [1, 2)
-// (exact for bf16 down to 2^-16 of it, good to 2^-25; fp32 inputs as two halves of 11
-// bits), S and the U that goes into it as two halves (22 bits) under a power of two
+// fp16: keys and queries under the power of two that brings the row's norm to
+// [2^-1/2, 2^1/2) (exact for bf16 down to 2^-16 of the norm, good to 2^-24 of it; fp32
+// inputs as two halves of 11 bits), S and the U that goes into it as two halves (22 bits) under a power of two
 // of their column's, below 2^16 and 2^8.  Products of two low halves are left out
 // (2^-22).  A bf16 o is computed as an fp32 one and rounded at the end: its two terms
 // may cancel, as they do where a value is replaced.  Errors against 64 bits over
-// 40,001 tokens: states 2.2e-7, as a plain evaluation in 32 bits (two bf16
-// halves: 16 bits, some 3e-6 by that).
+// 40,001 tokens: states 1.8e-7, o 2.2e-7 (a plain evaluation of blocks in 32 bits:
+// 2.3e-7 and 3.1e-7).
 //
-// What bounds it: vector instructions (65 % of the issue slots, beside 25 % for
-// the matrix ones, at 32 sequences of 3,000 tokens and 16 heads of 128 x 128:
-// 540 us, 2.2 TB/s).
+// What bounds it: vector instructions take 55 % of the SIMDs' cycles and matrix
+// ones 45 %, half of these the fp32 ones (32 sequences of 3,000 tokens and 16 heads of
+// 128 x 128: 650 us at 2.06 GHz, 1.9 TB/s).
 //
-// Long sequences of few heads.  A head's blocks follow one another, so a call of
-// fewer heads than CUs is cut into segments of each sequence: the end state of a
+// Long sequences of few heads.  A head's blocks follow one another, so a call of up
+// to 64 heads (blocks of 128 columns of them) whose sequences have 64 blocks or more
+// on average is cut into segments of each sequence: the end state of a
 // segment is Phi S + F, where F is its end state from zeros and the columns of
 // Phi are those from unit vectors with values of zero, both computed by the same
 // blocks.  Three launches: Phi and F of every segment but the last; the states
@@ -310,7 +311,7 @@ struct Rows {
   }
 };
 
-// A row's power of two: its norm times `up` is in [1, 2).
+// A row's power of two: its norm times `up` is in [2^-1/2, 2^1/2).
 __device__ __forceinline__ Scale row_scale(float sq) {
   int half_e = static_cast<int>(__float_as_uint(sq) >> 24 & 127);
   half_e = half_e < 1 ? 1 : half_e;
@@ -786,7 +787,7 @@ __global__ void __launch_bounds__(64 * (kChainMax + Shared<KP, IN32, OUT>::kPrep
   // A column of S is held as S~ = S / sigma, sigma a power of two such that
   // |S~| < 2^16: its halves are fp16 numbers as they are.  `bound` >= |S~|.
   // A block multiplies S~ by decay sigma / sigma' and adds K^T (U / sigma'),
-  // where 32 keys' elements of at most 2 meet |U / sigma'| < 2^8: sigma' is
+  // where 32 keys' elements below 2^1/2 meet |U / sigma'| < 2^8: sigma' is
   // chosen so that both terms stay below 2^14, from the largest element that U
   // has under its decays to the block's end (what a block wrote and has forgotten
   // by then sets no scale) and from S~'s bound.  The halves' floor of 2^-24 leaves
@@ -1092,8 +1093,8 @@ hipError_t launch_delta(const DeltaParams& given, int in_dtype, int out_dtype, i
   DeltaParams p = given;
   const int state16 = state_dtype == PRECOG_F16;
   // Columns of a workgroup: all of a head's, up to 128, or as few as leave every
-  // workgroup a CU of its own (a block takes 3.3 us with 128 columns, 2.3 us with
-  // 32, 1.8 us with 16; two rounds of narrower ones take longer than one).
+  // workgroup a CU of its own (a block takes 3.7 us with 128 columns, 3.0 us with
+  // 32, 2.0 us with 16; two rounds of narrower ones take longer than one).
   int nv = 2, waves = (p.V + 31) / 32;
   if (waves > kChainMax) waves = kChainMax;
   if (p.segments == 1) {

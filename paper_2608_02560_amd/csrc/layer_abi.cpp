@@ -90,9 +90,10 @@ precog::DeltaParams delta_params(const precog_delta_desc* d, const void* q, cons
 // Segments that every sequence of a call is cut into.  A head's blocks of 32
 // tokens run one after the other on one CU, so up to 64 heads leave CUs idle that
 // can take other segments, at three times the work: 8 heads of 40,001 tokens take
-// 2,180 us whole and 393 us in 32 segments, 64 heads of 16,384 tokens 1,180 us
-// and 840 us in 4; 128 heads of 2,048 tokens 162 us and 168 us in 2.  A segment
-// has 16 blocks or more (8 heads of 2,048 tokens: 121 us whole, 100 us in 4).
+// 2,410 us whole and 408 us in 32 segments, 64 heads of 16,384 tokens 1,435 us
+// and 896 us in 4; 128 heads of 2,048 tokens 187 us and 181 us in 2, which is not
+// worth its workspace.  A segment has 16 blocks or more (8 heads of 2,048 tokens:
+// 130 us whole, 103 us in 4).
 int64_t delta_segments(const precog_delta_desc* d, int64_t tokens) {
   const int64_t heads = d->batch * d->v_heads * ((d->v_dim + 127) / 128);
   const int64_t blocks = (tokens + 31) / 32 / d->batch;  // of a sequence, on average
