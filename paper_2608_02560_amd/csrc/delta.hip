@@ -9,11 +9,6 @@
 //   O = scale (diag(e^b) Q S + (G . Q K^T) U)
 //   S <- e^{b_end} S + K^T diag(e^{b_end - b}) U
 //
-// (the gate with the values, not with T: a closed one keeps a value out of X's
-// scale, however large) and, for keys of any length |k|, u' = |k| u in place of u:
-// with k^ = k / |k|, A_ij = beta_i |k_i|^2 G_ij k^_i.k^_j and X = diag(beta |k|) V -
-// diag(beta |k|^2 e^b) K^ S.
-//
 // so a block is a handful of small matrix products, and only those with S
 // depend on the block before.  One workgroup owns one head of one sequence (or
 // some of its columns: the columns of S and V do not meet).  Two kinds of
@@ -27,6 +22,11 @@
 //            wave, since a product's result lies in the registers as the next
 //            product wants its operand.
 //
+// Keys have any length: with |k| the power of two next to it (over what qk_norm
+// divides by), k^ = k / |k| and u' = |k| u in place of u, A_ij = beta_i |k_i|^2 G_ij
+// k^_i.k^_j and X = diag(beta |k|) V - diag(beta |k|^2 e^b) K^ S.
+// What a closed gate or a key of zeros keeps out, however large, is a zero of X.
+//
 // Operands.  v_mfma_f32_16x16x32_f16 takes rows (columns) l % 16 and the eight
 // depths 8 (l / 16) + j of its operands from lane l, and gives lane l the rows
 // 4 (l / 16) + r of column l % 16.  Two results of 16 rows are therefore one
@@ -39,13 +39,13 @@
 // values and key lengths make of them, and a token's small numbers are not to
 // depend on its neighbours' large ones.  The products with S and K have operands of
 // fp16: keys and queries under the power of two that brings the row's norm to
-// [2^-1/2, 2^1/2) (exact for bf16 down to 2^-16 of the norm, good to 2^-24 of it; fp32
-// inputs as two halves of 11 bits), S and the U that goes into it as two halves (22 bits) under a power of two
-// of their column's, below 2^16 and 2^8.  Products of two low halves are left out
-// (2^-22).  A bf16 o is computed as an fp32 one and rounded at the end: its two terms
-// may cancel, as they do where a value is replaced.  Errors against 64 bits over
-// 40,001 tokens: states 1.8e-7, o 2.2e-7 (a plain evaluation of blocks in 32 bits:
-// 2.3e-7 and 3.1e-7).
+// [2^-1/2, 2^1/2) (exact for bf16 down to 2^-16 of the norm, good to 2^-24 of it;
+// fp32 inputs as two halves of 11 bits), S and the U that goes into it as two halves
+// (22 bits) under a power of two of their column's, below 2^16 and 2^8.  Products of
+// two low halves are left out (2^-22).  A bf16 o is computed as an fp32 one and
+// rounded at the end: its two terms may cancel, as they do where a value is replaced.
+// Errors against 64 bits over 40,001 tokens: states 1.8e-7, o 2.2e-7 (a plain
+// evaluation of blocks in 32 bits: 2.3e-7 and 3.1e-7).
 //
 // What bounds it: vector instructions take 55 % of the SIMDs' cycles and matrix
 // ones 45 %, half of these the fp32 ones (32 sequences of 3,000 tokens and 16 heads of
@@ -120,10 +120,9 @@ struct Scratch {
 };
 
 // A and its inverse take the place of T's operands until these are made, tile by
-// tile.  Groups of four columns are
-// permuted within a row, so that 16 lanes that read a column of groups meet
-// different banks, and neighbouring rows of the last tile change places, so that
-// a row of it and the same one of the first do.
+// tile.  Groups of four columns are permuted within a row, so that 16 lanes that read
+// a column of groups meet different banks, and neighbouring rows of the last tile
+// change places, so that a row of it and the same one of the first do.
 __device__ __forceinline__ uint32_t a_at(uint32_t tile, uint32_t r, uint32_t c) {
   return 256 * tile + 16 * (r ^ tile / 2) + (4 * (c / 4 ^ r / 4) | c % 4);
 }
